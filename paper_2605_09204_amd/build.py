@@ -2,7 +2,8 @@
 
 Usage: ``python -m paper_2605_09204_amd.build`` (or ``build_library()``).
 Cross-compiles without a GPU.  Each translation unit under ``csrc/`` (one per
-arithmetic mode of the chain kernel, the carry/apply kernels, the host API) is
+arithmetic mode of the chain kernel, the carry/apply kernels, the region block's
+operators, the host API) is
 compiled in parallel, then linked.  Packed fp32 instructions are disabled for
 all device code.
 """
@@ -20,7 +21,12 @@ CSRC = os.path.join(PKG, "csrc")
 SOURCES = ["lbi_chain_f32.hip", "lbi_chain_f32x.hip", "lbi_chain_bf16.hip", "lbi_chain_bf16r1.hip",
            "lbi_chain_wave.hip", "lbi_chain_wide.hip",
            "lbi_chain_ksplit.hip", "lbi_tree.hip", "lbi_chain_ring.hip", "lbi_aux.hip", "lbi_norms.hip", "lbi_region.hip",
-           "lbi_api.hip"]
+           "lbi_rms.hip", "lbi_conv.hip", "lbi_ssm.hip", "lbi_ssm_backward.hip", "lbi_block_api.hip", "lbi_api.hip"]
+# Sources none of whose kernels may spill vector registers: their loads of partial rows branch by
+# lane, and hipcc has spilled inside such a branch only the lanes that take it, so that the
+# others came back with wrong values.  The build fails if one spills.
+NO_SPILLS = {"lbi_rms.hip", "lbi_conv.hip", "lbi_ssm.hip", "lbi_ssm_backward.hip"}
+_USAGE = "kernel-resource-usage"
 INCLUDE = os.path.join(ROOT, "include")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "liblbi.so")
@@ -56,12 +62,24 @@ def _run(cmd, verbose):
     return res.returncode, err
 
 
+def spills(remarks: str):
+    """The kernels that spill vector registers, from hipcc's resource remarks."""
+    found, name = [], "?"
+    for line in remarks.splitlines():
+        if "Function Name:" in line:
+            name = line.split("Function Name:")[1].split("[")[0].strip()
+        elif "VGPRs Spill:" in line and int(line.split("VGPRs Spill:")[1].split("[")[0]) > 0:
+            found.append(name)
+    return found
+
+
 def build_library(verbose: bool = False) -> str:
     """Compile the library (always recompiles) and return its path."""
     os.makedirs(LIBDIR, exist_ok=True)
     tag = f".tmp{os.getpid()}"
     objs = [os.path.join(LIBDIR, os.path.splitext(s)[0] + ".o" + tag) for s in SOURCES]
     cmds = [[hipcc()] + compile_flags() + ["-c", os.path.join(CSRC, s), "-o", o]
+            + ([f"-Rpass-analysis={_USAGE}"] if s in NO_SPILLS else [])
             for s, o in zip(SOURCES, objs)]
     try:
         with concurrent.futures.ThreadPoolExecutor(max_workers=len(cmds)) as ex:
@@ -69,7 +87,12 @@ def build_library(verbose: bool = False) -> str:
         for (rc, err), src in zip(results, SOURCES):
             if rc != 0:
                 raise RuntimeError(f"hipcc failed on {src} ({rc}):\n{err}")
-            if verbose and err.strip():
+            if src in NO_SPILLS:
+                if _USAGE not in err:
+                    raise RuntimeError(f"hipcc printed no resource usage for {src}")
+                if spills(err):
+                    raise RuntimeError(f"kernels of {src} spill registers: {spills(err)}")
+            elif verbose and err.strip():
                 print(err, file=sys.stderr)
         tmp = LIB + tag
         rc, err = _run([hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp] + objs,
