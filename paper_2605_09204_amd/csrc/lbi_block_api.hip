@@ -172,6 +172,15 @@ struct ScanTensors {
     }
 };
 
+// A tile's rows are addressed by 32-bit offsets in bytes.
+bool too_wide(std::initializer_list<int64_t> strides)
+{
+    for (int64_t ld : strides)
+        if (ld > LBI_SSM_MAX_LD)
+            return true;
+    return false;
+}
+
 bool too_many_groups(const SsmCut &c) { return c.ranges > (kMostGroups - 1) / c.tiles; }
 
 size_t scan_layout(SsmArgs &a, void *workspace)
@@ -444,7 +453,8 @@ lbi_status lbi_ssm_scan(const lbi_ssm_inputs *in, void *y, int64_t ld_y, float *
     a.state_out = state_out;
     a.slots = slots; a.n_slots = n_slots;
     a.cut = ssm_forward_cut(*in, in->offsets != nullptr);
-    if (too_many_groups(a.cut))
+    if (too_many_groups(a.cut) || too_wide({in->ld_u, in->ld_delta, in->z ? in->ld_z : 0, in->ld_B,
+                                            in->ld_C, ld_y}))
         return LBI_ERR_SHAPE;
     const size_t need = scan_layout(a, workspace);
     st = check_workspace(workspace, workspace_bytes, need);
@@ -515,7 +525,10 @@ lbi_status lbi_ssm_scan_backward(const lbi_ssm_inputs *in, const void *dy, int64
         a.out.dz = nullptr;
     a.cut = ssm_backward_cut(*in, in->offsets != nullptr);
     const size_t need = backward_layout(a, workspace);
-    if (too_many_groups(a.cut))
+    if (too_many_groups(a.cut) ||
+        too_wide({in->ld_u, in->ld_delta, in->z ? in->ld_z : 0, in->ld_B, in->ld_C, ld_dy,
+                  grads->ld_du, grads->ld_ddelta, in->z ? grads->ld_dz : 0, grads->ld_dB,
+                  grads->ld_dC}))
         return LBI_ERR_SHAPE;
     st = check_workspace(workspace, workspace_bytes, need);
     if (st != LBI_OK)

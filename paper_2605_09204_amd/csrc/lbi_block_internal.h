@@ -72,8 +72,8 @@ struct SsmCut {
     int32_t tiles;  // workgroups along the channels, over all groups
     bool joined;    // states pass between ranges
 };
-SsmCut ssm_cut(int64_t T, int64_t sequences, int32_t D, int32_t G, bool ragged, int64_t blocks,
-               int32_t least);
+SsmCut ssm_cut(int64_t T, int64_t sequences, int32_t D, int32_t G, bool ragged, double again,
+               double launches);
 
 struct SsmArgs {
     lbi_ssm_inputs in;

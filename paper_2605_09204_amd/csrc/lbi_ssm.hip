@@ -24,24 +24,26 @@ constexpr int kTile = 32;  // tokens staged at a time
 // state (state_out may be state_in), so the first walk's copy is read.
 template <int NS>
 __device__ __forceinline__ void begin_states(const SsmArgs &a, const Segment &seg, int64_t r,
-                                             int64_t t1, int64_t dn, int nn, float (&h)[NS])
+                                             int64_t t1, uint32_t dn, int nn, float (&h)[NS])
 {
     const int64_t dN = (int64_t)a.in.D * a.in.N;
     if (!a.in.state_in) {
         zero_states(h);
     } else if (a.cut.joined && seg.end > t1) {
-        load_states<NS>(a.starts + r * dN + dn, nn, h);
+        load_states<NS>(part_of(a.starts + r * dN, dn), nn, h);
     } else {
         const int64_t row = state_row(a.slots, a.n_slots, seg.seq);
-        load_states<NS>(a.in.state_in + (row < 0 ? 0 : row) * dN + dn, row < 0 ? 0 : nn, h);
+        load_states<NS>(part_of(a.in.state_in + (row < 0 ? 0 : row) * dN, dn), row < 0 ? 0 : nn, h);
     }
 }
 
 // ENDS: the first walk.  Otherwise the one that writes y and state_out.
 template <typename T, int NS, bool ENDS>
-__global__ __launch_bounds__(256) void scan_kernel(const SsmArgs a)
+__global__ __launch_bounds__(256, NS <= 4 ? 4 : 2) void scan_kernel(const SsmArgs a)
 {
     constexpr int NP = 4 * NS, E = NS >= 2 ? NS / 2 : 1;
+    constexpr int BROWS = 256 / NP;  // rows of B and C that the workgroup stages at once
+    constexpr int UNROLL = NS <= 4 ? 2 : 1;
     __shared__ __align__(16) f2 dx[kTile][kChannels];
     __shared__ __align__(16) float bc[kTile][4][2 * NS];
     __shared__ __align__(16) float ys[ENDS ? 1 : kTile][kPitch];
@@ -53,7 +55,7 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsmArgs a)
     const int c = (tid >> 6) * 16 + (lane & 15);
     const int nn = c < tile.left ? in.N - g * NS : 0;  // states that this lane holds (at most NS)
     const int64_t dN = (int64_t)in.D * in.N;
-    const int64_t dn = (int64_t)(tile.d0 + c) * in.N + g * NS;
+    const uint32_t dn = (uint32_t)((tile.d0 + c) * in.N + g * NS) * 4u;  // bytes
     int64_t t0, t1;
     range_rows(a.cut, q, r, &t0, &t1);
 
@@ -64,8 +66,9 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsmArgs a)
             if (row < 0)
                 continue;
             float h[NS];
-            load_states<NS>(in.state_in + (in.state_in ? row * dN + dn : 0), in.state_in ? nn : 0, h);
-            store_states<NS>(a.state_out + row * dN + dn, nn, h);
+            load_states<NS>(part_of(in.state_in + (in.state_in ? row * dN : 0), dn), in.state_in ? nn : 0,
+                            h);
+            store_states<NS>(part_of(a.state_out + row * dN, dn), nn, h);
         }
     }
     if (t0 >= t1)
@@ -86,19 +89,20 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsmArgs a)
             t = seg.start;
             if (in.state_in) {
                 const int64_t row = state_row(a.slots, a.n_slots, seg.seq);
-                load_states<NS>(in.state_in + (row < 0 ? 0 : row) * dN + dn, row < 0 ? 0 : nn, h);
-                store_states<NS>(a.starts + r * dN + dn, nn, h);
+                load_states<NS>(part_of(in.state_in + (row < 0 ? 0 : row) * dN, dn), row < 0 ? 0 : nn,
+                                h);
+                store_states<NS>(part_of(a.starts + r * dN, dn), nn, h);
             }
         }
     } else {
         seg.enter(q, t0);
         if (seg.start < t0)
-            load_states<NS>(a.ends + (r - 1) * dN + dn, nn, h);
+            load_states<NS>(part_of(a.ends + (r - 1) * dN, dn), nn, h);
         else
             begin_states<NS>(a, seg, r, t1, dn, nn, h);
     }
     float A2[NS];
-    load_states<NS>(in.A + dn, nn, A2);
+    load_states<NS>(part_of(in.A, dn), nn, A2);
 #pragma unroll
     for (int i = 0; i < NS; ++i)
         A2[i] *= kLog2e;
@@ -111,21 +115,22 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsmArgs a)
     load_some<8>(in.skip + (in.skip ? d8 : 0), in.skip && !ENDS ? left : 0, skip);
     Raw<T, 8> ru, rd, rz;
     T rb[E], rc[E];
+    const int br = tid / NP, bn = tid % NP, bcol = tile.group * in.N + bn;
+    const Plane<T> pu(in.u, in.ld_u, row, d8), pd(in.delta, in.ld_delta, row, d8),
+        pz(in.z, in.ld_z, row, d8), py(a.y, a.ld_y, row, d8), pb(in.B, in.ld_B, br, bcol),
+        pc(in.C, in.ld_C, br, bcol);
     auto load = [&](int64_t at, int n) {
-        const int64_t k = at + row;
         const int m = row < n ? left : 0;
-        ru.load((const T *)in.u + k * in.ld_u + d8, m);
-        rd.load((const T *)in.delta + k * in.ld_delta + d8, m);
+        ru.load(pu.at(at), m);
+        rd.load(pd.at(at), m);
         if (!ENDS && in.z)
-            rz.load((const T *)in.z + k * in.ld_z + d8, m);
+            rz.load(pz.at(at), m);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int i = tid + e * 256, br = i / NP, bn = i % NP;
-            const bool there = br < n && bn < in.N;
-            const int64_t k = at + br, o = (int64_t)tile.group * in.N + bn;
-            rb[e] = there ? ((const T *)in.B)[k * in.ld_B + o] : T(0);
+            const bool there = br + e * BROWS < n && bn < in.N;
+            rb[e] = there ? *pb.at(at + e * BROWS) : T(0);
             if (!ENDS)
-                rc[e] = there ? ((const T *)in.C)[k * in.ld_C + o] : T(0);
+                rc[e] = there ? *pc.at(at + e * BROWS) : T(0);
         }
     };
     auto tile_rows = [&](const Segment &s, int64_t at) {
@@ -142,20 +147,23 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsmArgs a)
             ru.unpack(u);
             rd.unpack(d);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float v = d[i] + bias[i];
-                if (in.softplus)
-                    v = softplus(v);
-                v = row < n ? v : 0.f;
-                dx[row][ch + i] = f2{v, v * u[i]};
+            for (int i = 0; i < 8; ++i)
+                d[i] += bias[i];
+            steps_of<8>(in.softplus, d);
+            if (row >= n) {  // rows past the tile's last one change nothing
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    d[i] = u[i] = 0.f;
             }
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int i = tid + e * 256, br = i / NP, bn = i % NP;
-                if (NS > 1 || i < kTile * NP) {
-                    bc[br][bn / NS][bn % NS] = widen(rb[e]);
+            for (int i = 0; i < 8; ++i)
+                dx[row][ch + i] = f2{d[i], d[i] * u[i]};
+            if (NS > 1 || br < kTile) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    bc[br + e * BROWS][bn / NS][bn % NS] = widen(rb[e]);
                     if (!ENDS)
-                        bc[br][bn / NS][NS + bn % NS] = widen(rc[e]);
+                        bc[br + e * BROWS][bn / NS][NS + bn % NS] = widen(rc[e]);
                 }
             }
         }
@@ -171,36 +179,39 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsmArgs a)
             n = tile_rows(seg, t);
             load(t, n);
         }
-        for (int k = 0; k < rows; k += 4) {
-            float y[4];
+        for (int k0 = 0; k0 < rows; k0 += 4 * UNROLL) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const f2 p = dx[k + j][c];
-                float b[NS], cc[NS];
+            for (int k = k0; k < k0 + 4 * UNROLL; k += 4) {
+                float y[4];
 #pragma unroll
-                for (int i = 0; i < NS; ++i) {
-                    b[i] = bc[k + j][g][i];
-                    if (!ENDS)
-                        cc[i] = bc[k + j][g][NS + i];
+                for (int j = 0; j < 4; ++j) {
+                    const f2 p = dx[k + j][c];
+                    float b[NS], cc[NS];
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) {
+                        b[i] = bc[k + j][g][i];
+                        if (!ENDS)
+                            cc[i] = bc[k + j][g][NS + i];
+                    }
+                    if (ENDS)
+                        total += p.x;
+                    y[j] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) {
+                        h[i] = fmaf(__builtin_amdgcn_exp2f(p.x * A2[i]), h[i], p.y * b[i]);
+                        if (!ENDS)
+                            y[j] = fmaf(cc[i], h[i], y[j]);
+                    }
                 }
-                if (ENDS)
-                    total += p.x;
-                y[j] = 0.f;
-#pragma unroll
-                for (int i = 0; i < NS; ++i) {
-                    h[i] = fmaf(__builtin_amdgcn_exp2f(p.x * A2[i]), h[i], p.y * b[i]);
-                    if (!ENDS)
-                        y[j] = fmaf(cc[i], h[i], y[j]);
-                }
+                if (!ENDS)
+                    ys[k + g][c] = sum_states(y);
             }
-            if (!ENDS)
-                ys[k + g][c] = sum_states(y);
         }
         if (!ENDS && ended) {
             if (a.state_out) {
                 const int64_t to = state_row(a.slots, a.n_slots, was.seq);
                 if (to >= 0)
-                    store_states<NS>(a.state_out + to * dN + dn, nn, h);
+                    store_states<NS>(part_of(a.state_out + to * dN, dn), nn, h);
             }
             if (more)
                 begin_states<NS>(a, seg, r, t1, dn, nn, h);
@@ -217,13 +228,13 @@ __global__ __launch_bounds__(256) void scan_kernel(const SsmArgs a)
                 for (int i = 0; i < 8; ++i)
                     y[i] *= silu(zz[i]);
             }
-            store_some<8>((T *)a.y + (at + row) * a.ld_y + d8, left, y);
+            store_some<8>(py.at(at), left, y);
         }
         if (!more)
             break;
     }
     if (ENDS) {
-        store_states<NS>(a.ends + r * dN + dn, nn, h);
+        store_states<NS>(part_of(a.ends + r * dN, dn), nn, h);
         if (g == 0 && c < tile.left)
             a.sums[r * in.D + tile.d0 + c] = total;
     }
@@ -288,7 +299,7 @@ template <typename T> hipError_t forward(const SsmArgs &a, hipStream_t stream)
             scan_kernel<T, NS, true><<<grid, 256, 0, stream>>>(a);
             hipError_t e = hipGetLastError();
             if (e == hipSuccess)
-                e = launch_carry(a, a.ends, a.sums, false, stream);
+                e = launch_carry(a, stream);
             if (e != hipSuccess)
                 return e;
         }
@@ -316,36 +327,52 @@ template <typename T> hipError_t step(const SsmArgs &a, hipStream_t stream)
 
 }  // namespace
 
-// Ranges so that about `blocks` workgroups exist, of at least `least` tokens and
-// a multiple of that.
-SsmCut ssm_cut(int64_t T, int64_t sequences, int32_t D, int32_t G, bool ragged, int64_t blocks,
-               int32_t least)
+// The cut of least cost.  A range's time goes by its tokens, and by how many
+// workgroups share its CU: measured on the scan of 16384 tokens, 1536 channels and 16 states
+// (192 to 3072 workgroups), one of m alike takes 0.4 + 0.55 m of what it takes alone.
+// Joined ranges add `again` of that work (the first walk skips one range a
+// sequence) and launches worth `launches` tokens; START tokens stand for a
+// workgroup's beginning.  Ranges are whole tiles of at least `least` tokens.
+SsmCut ssm_cut(int64_t T, int64_t sequences, int32_t D, int32_t G, bool ragged, double again,
+               double launches)
 {
+    constexpr double START = 16;
+    constexpr int64_t CUS = 256;
     SsmCut c;
     c.tiles = G * ((D / G + kChannels - 1) / kChannels);
     const int64_t rows = ragged || sequences == 0 ? T : T / sequences;
     const int64_t many = ragged || sequences == 0 ? 1 : sequences;
-    int64_t parts = blocks / (many * c.tiles);
-    if (parts < 1)
-        parts = 1;
-    int64_t tokens = (rows + parts - 1) / parts;
-    tokens = (tokens + least - 1) / least * least;
-    c.tokens = tokens > 0 ? tokens : least;
-    parts = (rows + c.tokens - 1) / c.tokens;
-    if (parts < 1)
-        parts = 1;
-    c.per_sequence = ragged ? 0 : (int32_t)parts;
-    c.ranges = parts * many;
-    c.joined = parts > 1;
+    const int64_t base = many * c.tiles;
+    // Sequences of lengths of their own may be short, and a tile holds one
+    // sequence: shorter ranges keep the worst case short.
+    const int64_t least = ragged ? kTile : 2 * kTile;
+    int64_t best = 1, best_tokens = rows;
+    double best_cost = 1e300;
+    for (int64_t p = 1; p == 1 || (p <= rows / least && base * p <= 16 * CUS);
+         p += 1 + p / 8) {
+        int64_t tokens = (rows + p - 1) / p;
+        tokens = (tokens + kTile - 1) / kTile * kTile;
+        const int64_t parts = tokens > 0 ? (rows + tokens - 1) / tokens : 1;
+        const double m = (double)((base * parts + CUS - 1) / CUS);
+        double cost = ((double)tokens + START) * (0.4 + 0.55 * m);
+        if (parts > 1)
+            cost = cost * (1.0 + again * (double)(parts - 1) / (double)parts) + launches;
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = parts;
+            best_tokens = tokens;
+        }
+    }
+    c.tokens = best_tokens > 0 ? best_tokens : kTile;
+    c.per_sequence = ragged ? 0 : (int32_t)best;
+    c.ranges = best * many;
+    c.joined = best > 1;
     return c;
 }
 
-// Workgroups wanted: four a CU, as many as run at once.  Ranges of 32 tokens at
-// least when sequences have lengths of their own (a range may hold many short
-// ones), otherwise of 64: two tiles, so that loads overlap the walk.
 SsmCut ssm_forward_cut(const lbi_ssm_inputs &in, bool ragged)
 {
-    return ssm_cut(in.T, in.sequences, in.D, in.G, ragged, 1024, ragged ? kTile : 2 * kTile);
+    return ssm_cut(in.T, in.sequences, in.D, in.G, ragged, 0.75, 64);
 }
 
 hipError_t launch_ssm_scan(const SsmArgs &a, hipStream_t stream)

@@ -17,27 +17,60 @@ namespace {
 constexpr int kChannels = 64;   // of a workgroup
 constexpr int kPitch = 80;      // floats a row of an LDS plane that lane rows write
 
-// log(1 + e^v), relative error a few 2^-24 everywhere: with e = e^-|v| it is
-// max(v, 0) + log1p(e), and log1p(e) = 2 atanh(e / (2 + e)), whose series in
-// s = e / (2 + e) <= 1/3 is cut at s^15 (the next term is 2e-9 of the sum).
+// log(1 + e^v) = max(v, 0) + log1p(e), e = e^-|v|.  With w = 1 + e rounded,
+// log1p(e) = log(w) + (e - (w - 1)) to first order in what the rounding lost, which
+// keeps the relative error at a few 2^-24 where e is small.  NaN gives NaN.
 __device__ __forceinline__ float softplus(float v)
 {
-    const float x = -fminf(fabsf(v), 120.f);
-    const float p = x * kLog2e;
-    const float r = fmaf(x, kLog2e, -p);  // what the product lost
-    const float q = __builtin_amdgcn_exp2f(p);
-    const float e = fmaf(q * kLn2, r, q);
-    const float s = e * __builtin_amdgcn_rcpf(2.f + e), s2 = s * s;
-    float l = 1.f / 15.f;
-    l = fmaf(l, s2, 1.f / 13.f);
-    l = fmaf(l, s2, 1.f / 11.f);
-    l = fmaf(l, s2, 1.f / 9.f);
-    l = fmaf(l, s2, 1.f / 7.f);
-    l = fmaf(l, s2, 1.f / 5.f);
-    l = fmaf(l, s2, 1.f / 3.f);
-    l = fmaf(l * s2, s, s);
-    const float y = fmaf(2.f, l, fmaxf(v, 0.f));
-    return v != v ? v : y;
+    const float e = __builtin_amdgcn_exp2f(-fabsf(v) * kLog2e);
+    const float w = 1.f + e;
+    return fmaf(__builtin_amdgcn_logf(w), kLn2, e - (w - 1.f)) + fmaxf(v, 0.f);
+}
+
+// The steps D_t of V channels from delta + delta_bias.  (The choice stands outside
+// the loop: V chains of dependent operations at once.)
+template <int V> __device__ __forceinline__ void steps_of(bool use_softplus, float (&d)[V])
+{
+    if (use_softplus) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            d[i] = softplus(d[i]);
+    }
+}
+
+// The address of a uniform one plus this lane's 32-bit offset.  The offset is made
+// opaque at each use: the compiler would otherwise form the sum with the loop's
+// invariant part ahead of the loop, two registers for every tensor.
+template <typename T> __device__ __forceinline__ T *lane_address(T *uniform, uint32_t bytes)
+{
+    asm volatile("" : "+v"(bytes));
+    return (T *)((char *)uniform + bytes);
+}
+
+// A value that is formed here, not where it is used (the compiler would sink sums
+// that nothing reads until a walk's end past the walk, and keep their terms).
+__device__ __forceinline__ void pin(float &x) { asm volatile("" : "+v"(x)); }
+
+// A token tensor as a staging thread sees it: the rows of a tile begin at a uniform
+// address, its own part of them at a 32-bit offset from there (row strides are
+// limited to that end).
+template <typename T> struct Plane {
+    T *base;
+    int64_t ld;
+    uint32_t offset;  // bytes
+    __device__ __forceinline__ Plane(const void *p, int64_t stride, int row, int col)
+        : base((T *)p), ld(stride), offset((uint32_t)((row * (int)stride + col) * (int)sizeof(T)))
+    {
+    }
+    __device__ __forceinline__ T *at(int64_t t) const
+    {
+        return lane_address(base + t * ld, offset);
+    }
+};
+// The same for arrays [.][D][N] of states: `bytes` is the thread's own part.
+__device__ __forceinline__ float *part_of(const float *uniform, uint32_t bytes)
+{
+    return lane_address((float *)uniform, bytes);
 }
 
 __device__ __forceinline__ Sequences ssm_sequences(const lbi_ssm_inputs &in)
@@ -124,22 +157,23 @@ __device__ __forceinline__ float sum_states(const float (&v)[4])
     return add_rows<16>(even, odd);
 }
 
-// The states at the ranges' ends (or, REVERSE, the gradients at their starts),
+// The states at the ranges' ends (and, with `heads`, the gradients at their starts),
 // each as if its range had been entered with zeros, made whole in place along
-// the ranges that follow each other: one thread a channel and state.
-template <bool REVERSE>
-__global__ __launch_bounds__(256) void carry_kernel(const SsmArgs a, float *ends,
-                                                    const float *sums)
+// the ranges that follow each other: one thread a channel and state.  A thread has
+// the ends of DEEP ranges in flight: its time is that many fewer trips to memory.
+template <int DEEP>
+__global__ __launch_bounds__(256) void carry_kernel(const SsmArgs a)
 {
-    constexpr int DEEP = 8;  // ranges loaded ahead
     const int64_t dN = (int64_t)a.in.D * a.in.N;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= dN)
         return;
+    const bool reverse = blockIdx.z == 1;
     const int64_t d = i / a.in.N;
     const int64_t count = a.cut.per_sequence > 0 ? a.cut.per_sequence : a.cut.ranges;
     const int64_t first = (int64_t)blockIdx.y * count;
-    const int32_t stops = REVERSE ? kEnds : kStarts;
+    const int32_t stops = reverse ? kEnds : kStarts;
+    float *ends = reverse ? a.heads : a.ends;
     const float A2 = a.in.A[i] * kLog2e;
     float cur = 0.f;
     for (int64_t k = 0; k < count; k += DEEP) {
@@ -147,33 +181,32 @@ __global__ __launch_bounds__(256) void carry_kernel(const SsmArgs a, float *ends
         int32_t f[DEEP];
 #pragma unroll
         for (int j = 0; j < DEEP; ++j) {
-            if (k + j < count) {
-                const int64_t r = first + (REVERSE ? count - 1 - (k + j) : k + j);
-                e[j] = ends[r * dN + i];
-                w[j] = sums[r * a.in.D + d];
-                f[j] = a.flags[r];
-            }
+            // (past the last range the last one again: nothing is stored then)
+            const int64_t at = k + j < count ? k + j : count - 1;
+            const int64_t r = first + (reverse ? count - 1 - at : at);
+            e[j] = ends[r * dN + i];
+            w[j] = a.sums[r * a.in.D + d];
+            f[j] = a.flags[r];
         }
 #pragma unroll
         for (int j = 0; j < DEEP; ++j) {
             if (k + j < count) {
-                const int64_t r = first + (REVERSE ? count - 1 - (k + j) : k + j);
+                const int64_t r = first + (reverse ? count - 1 - (k + j) : k + j);
                 cur = f[j] & stops ? e[j] : fmaf(__builtin_amdgcn_exp2f(A2 * w[j]), cur, e[j]);
                 ends[r * dN + i] = cur;
             }
         }
     }
 }
-inline hipError_t launch_carry(const SsmArgs &a, float *ends, const float *sums, bool reverse,
-                               hipStream_t stream)
+inline hipError_t launch_carry(const SsmArgs &a, hipStream_t stream)
 {
     const int64_t dN = (int64_t)a.in.D * a.in.N;
     const int64_t chains = a.cut.per_sequence > 0 ? a.cut.ranges / a.cut.per_sequence : 1;
-    const dim3 grid((unsigned)((dN + 255) / 256), (unsigned)chains);
-    if (reverse)
-        carry_kernel<true><<<grid, 256, 0, stream>>>(a, ends, sums);
+    const dim3 grid((unsigned)((dN + 255) / 256), (unsigned)chains, a.heads ? 2 : 1);
+    if (a.cut.ranges / chains <= 8)
+        carry_kernel<8><<<grid, 256, 0, stream>>>(a);
     else
-        carry_kernel<false><<<grid, 256, 0, stream>>>(a, ends, sums);
+        carry_kernel<32><<<grid, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 

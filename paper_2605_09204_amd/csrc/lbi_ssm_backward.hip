@@ -29,15 +29,16 @@ namespace lbi {
 namespace {
 
 // Tokens between marks, and whether their decays stay in registers too.
-constexpr int step_of(int NS) { return NS <= 4 ? 16 : (NS == 8 ? 8 : 4); }
-constexpr bool keeps_decays(int NS) { return NS <= 2; }
+constexpr int step_of(int NS) { return NS <= 8 ? 8 : 4; }
+constexpr bool keeps_decays(int NS) { return NS <= 4; }
 constexpr int kSweep = 32;  // tokens that the first walk stages at a time
 
 // The first walk.  JOINED: ranges are entered in their middle.
 template <typename T, int NS, bool JOINED>
-__global__ __launch_bounds__(256) void sweep_kernel(const SsmArgs a)
+__global__ __launch_bounds__(256, NS <= 2 ? 4 : (NS == 4 ? 3 : (NS == 8 ? 2 : 1))) void sweep_kernel(const SsmArgs a)
 {
     constexpr int NP = 4 * NS, E = NS >= 2 ? NS / 2 : 1, STEP = step_of(NS);
+    constexpr int BROWS = 256 / NP;  // rows of B and C that the workgroup stages at once
     __shared__ __align__(16) f2 dx[kSweep][kChannels];
     __shared__ __align__(16) float bc[kSweep][4][2 * NS];
     __shared__ float es[JOINED ? kSweep : 1][kChannels];
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(256) void sweep_kernel(const SsmArgs a)
     const int c = (tid >> 6) * 16 + (lane & 15);
     const int nn = c < tile.left ? in.N - g * NS : 0;
     const int64_t dN = (int64_t)in.D * in.N;
-    const int64_t dn = (int64_t)(tile.d0 + c) * in.N + g * NS;
+    const uint32_t dn = (uint32_t)((tile.d0 + c) * in.N + g * NS) * 4u;  // bytes
     int64_t t0, t1;
     range_rows(a.cut, q, r, &t0, &t1);
     if (t0 >= t1)
@@ -63,13 +64,13 @@ __global__ __launch_bounds__(256) void sweep_kernel(const SsmArgs a)
     zero_states(h);
     auto begin = [&]() {
         if (in.state_in)
-            load_states<NS>(in.state_in + seg.seq * dN + dn, nn, h);
+            load_states<NS>(part_of(in.state_in + seg.seq * dN, dn), nn, h);
         else
             zero_states(h);
     };
     if (!entered)
         begin();
-    load_states<NS>(in.A + dn, nn, A2);
+    load_states<NS>(part_of(in.A, dn), nn, A2);
 #pragma unroll
     for (int i = 0; i < NS; ++i)
         A2[i] *= kLog2e;
@@ -87,24 +88,25 @@ __global__ __launch_bounds__(256) void sweep_kernel(const SsmArgs a)
     load_some<8>(in.delta_bias + (in.delta_bias ? d8 : 0), in.delta_bias ? left : 0, bias);
     Raw<T, 8> ru, rd, rz, re;
     T rb[E], rc[E];
+    const int br = tid / NP, bn = tid % NP, bcol = tile.group * in.N + bn;
+    const Plane<T> pu(in.u, in.ld_u, row, d8), pd(in.delta, in.ld_delta, row, d8),
+        pz(in.z, in.ld_z, row, d8), pe(a.dy, a.ld_dy, row, d8), pb(in.B, in.ld_B, br, bcol),
+        pc(in.C, in.ld_C, br, bcol);
     auto load = [&](int64_t at, int n, bool heads) {
-        const int64_t k = at + row;
         const int m = row < n ? left : 0;
-        ru.load((const T *)in.u + k * in.ld_u + d8, m);
-        rd.load((const T *)in.delta + k * in.ld_delta + d8, m);
+        ru.load(pu.at(at), m);
+        rd.load(pd.at(at), m);
         if (JOINED && heads) {
-            re.load((const T *)a.dy + k * a.ld_dy + d8, m);
+            re.load(pe.at(at), m);
             if (in.z)
-                rz.load((const T *)in.z + k * in.ld_z + d8, m);
+                rz.load(pz.at(at), m);
         }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int i = tid + e * 256, br = i / NP, bn = i % NP;
-            const bool there = br < n && bn < in.N;
-            const int64_t k = at + br, o = (int64_t)tile.group * in.N + bn;
-            rb[e] = there ? ((const T *)in.B)[k * in.ld_B + o] : T(0);
+            const bool there = br + e * BROWS < n && bn < in.N;
+            rb[e] = there ? *pb.at(at + e * BROWS) : T(0);
             if (JOINED && heads)
-                rc[e] = there ? ((const T *)in.C)[k * in.ld_C + o] : T(0);
+                rc[e] = there ? *pc.at(at + e * BROWS) : T(0);
         }
     };
     auto tile_rows = [&](int64_t at) {
@@ -120,13 +122,17 @@ __global__ __launch_bounds__(256) void sweep_kernel(const SsmArgs a)
             ru.unpack(u);
             rd.unpack(d);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float v = d[i] + bias[i];
-                if (in.softplus)
-                    v = softplus(v);
-                v = row < n ? v : 0.f;
-                dx[row][ch + i] = f2{v, v * u[i]};
+            for (int i = 0; i < 8; ++i)
+                d[i] += bias[i];
+            steps_of<8>(in.softplus, d);
+            if (row >= n) {  // rows past the tile's last one change nothing
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    d[i] = u[i] = 0.f;
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                dx[row][ch + i] = f2{d[i], d[i] * u[i]};
             if (JOINED && first) {
                 float e[8], z[8];
                 re.unpack(e);
@@ -140,13 +146,12 @@ __global__ __launch_bounds__(256) void sweep_kernel(const SsmArgs a)
                 for (int i = 0; i < 8; ++i)
                     es[row][ch + i] = e[i];
             }
+            if (NS > 1 || br < kSweep) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int i = tid + e * 256, br = i / NP, bn = i % NP;
-                if (NS > 1 || i < kSweep * NP) {
-                    bc[br][bn / NS][bn % NS] = widen(rb[e]);
+                for (int e = 0; e < E; ++e) {
+                    bc[br + e * BROWS][bn / NS][bn % NS] = widen(rb[e]);
                     if (JOINED && first)
-                        bc[br][bn / NS][NS + bn % NS] = widen(rc[e]);
+                        bc[br + e * BROWS][bn / NS][NS + bn % NS] = widen(rc[e]);
                 }
             }
         }
@@ -170,7 +175,7 @@ __global__ __launch_bounds__(256) void sweep_kernel(const SsmArgs a)
         for (int k = 0; k < rows; k += 4) {
             if ((k % STEP) == 0 && at + k > begun) {
                 const int64_t m = (at + k) / STEP;
-                store_states<NS>(a.marks + m * dN + dn, nn, h);
+                store_states<NS>(part_of(a.marks + m * dN, dn), nn, h);
                 if (JOINED && open && g == 0 && c < tile.left)
                     a.mark_sums[m * in.D + tile.d0 + c] = total;
             }
@@ -201,7 +206,7 @@ __global__ __launch_bounds__(256) void sweep_kernel(const SsmArgs a)
         }
         if (JOINED && ended && heads && a.dstate_out) {
             float e[NS];
-            load_states<NS>(a.dstate_out + seq * dN + dn, nn, e);
+            load_states<NS>(part_of(a.dstate_out + seq * dN, dn), nn, e);
 #pragma unroll
             for (int i = 0; i < NS; ++i)
                 head[i] = fmaf(way[i], e[i], head[i]);
@@ -217,8 +222,8 @@ __global__ __launch_bounds__(256) void sweep_kernel(const SsmArgs a)
     if (JOINED) {
         // a range that no sequence enters sends no gradient back, one that none
         // leaves no state on: what is stored then is not used
-        store_states<NS>(a.ends + r * dN + dn, nn, h);
-        store_states<NS>(a.heads + r * dN + dn, nn, head);
+        store_states<NS>(part_of(a.ends + r * dN, dn), nn, h);
+        store_states<NS>(part_of(a.heads + r * dN, dn), nn, head);
         if (g == 0 && c < tile.left)
             a.sums[r * in.D + tile.d0 + c] = total;
         if (tid == 0 && tile.tile == 0 && tile.group == 0)
@@ -228,11 +233,12 @@ __global__ __launch_bounds__(256) void sweep_kernel(const SsmArgs a)
 
 // The second walk.
 template <typename T, int NS, bool JOINED>
-__global__ __launch_bounds__(256, NS <= 4 ? 2 : 1) void gradient_kernel(const SsmArgs a)
+__global__ __launch_bounds__(256, NS <= 4 ? 3 : 2) void gradient_kernel(const SsmArgs a)
 {
     constexpr int STEP = step_of(NS), NP = 4 * NS;
     constexpr int V = STEP <= 8 ? 2 : 4;             // channels a thread stages
     constexpr int E = (STEP * NP + 255) / 256;       // B (and C) values a thread stages
+    constexpr int BROWS = 256 / NP;                  // rows of them staged at once
     constexpr int PER = NS <= 2 ? 4 : (NS == 4 ? 2 : 1);  // tokens whose dB, dC are summed at once
     constexpr int LIVE = PER * NS * 2;               // their values in a lane: 16, or 8 and 32 at the ends
     constexpr bool KEEP = keeps_decays(NS);
@@ -253,7 +259,7 @@ __global__ __launch_bounds__(256, NS <= 4 ? 2 : 1) void gradient_kernel(const Ss
     const int c = wave * 16 + (lane & 15);
     const int nn = c < tile.left ? in.N - g * NS : 0;
     const int64_t dN = (int64_t)in.D * in.N;
-    const int64_t dn = (int64_t)(tile.d0 + c) * in.N + g * NS;
+    const uint32_t dn = (uint32_t)((tile.d0 + c) * in.N + g * NS) * 4u;  // bytes
     int64_t t0, t1;
     range_rows(a.cut, q, r, &t0, &t1);
     if (a.out.dstate_in && (in.offsets || in.T == 0)) {
@@ -262,15 +268,15 @@ __global__ __launch_bounds__(256, NS <= 4 ? 2 : 1) void gradient_kernel(const Ss
             if (q.at(s + 1) > q.at(s))
                 continue;
             float e[NS];
-            load_states<NS>(a.dstate_out + (a.dstate_out ? s * dN + dn : 0), a.dstate_out ? nn : 0,
-                            e);
-            store_states<NS>(a.out.dstate_in + s * dN + dn, nn, e);
+            load_states<NS>(part_of(a.dstate_out + (a.dstate_out ? s * dN : 0), dn),
+                            a.dstate_out ? nn : 0, e);
+            store_states<NS>(part_of(a.out.dstate_in + s * dN, dn), nn, e);
         }
     }
     if (t0 >= t1)
         return;  // only without tokens at all, when the sums have no rows
     float A2[NS], dA[NS], gr[NS], hs[STEP + 1][NS];
-    load_states<NS>(in.A + dn, nn, A2);
+    load_states<NS>(part_of(in.A, dn), nn, A2);
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
         A2[i] *= kLog2e;
@@ -289,21 +295,22 @@ __global__ __launch_bounds__(256, NS <= 4 ? 2 : 1) void gradient_kernel(const Ss
     __syncthreads();
     Raw<T, V> ru, rd, rz, re;
     T rb[E], rc[E];
+    const int br = tid / NP, bn = tid % NP, bcol = tile.group * in.N + bn;
+    const Plane<T> pu(in.u, in.ld_u, row, dv), pd(in.delta, in.ld_delta, row, dv),
+        pz(in.z, in.ld_z, row, dv), pe(a.dy, a.ld_dy, row, dv), pb(in.B, in.ld_B, br, bcol),
+        pc(in.C, in.ld_C, br, bcol);
     auto load = [&](int64_t at, int n) {
-        const int64_t k = at + row;
         const int m = row < n ? left : 0;
-        ru.load((const T *)in.u + k * in.ld_u + dv, m);
-        rd.load((const T *)in.delta + k * in.ld_delta + dv, m);
-        re.load((const T *)a.dy + k * a.ld_dy + dv, m);
+        ru.load(pu.at(at), m);
+        rd.load(pd.at(at), m);
+        re.load(pe.at(at), m);
         if (in.z)
-            rz.load((const T *)in.z + k * in.ld_z + dv, m);
+            rz.load(pz.at(at), m);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int i = tid + e * 256, br = i / NP, bn = i % NP;
-            const bool there = br < n && bn < in.N;
-            const int64_t k = at + br, o = (int64_t)tile.group * in.N + bn;
-            rb[e] = there ? ((const T *)in.B)[k * in.ld_B + o] : T(0);
-            rc[e] = there ? ((const T *)in.C)[k * in.ld_C + o] : T(0);
+            const bool there = br + e * BROWS < n && bn < in.N;
+            rb[e] = there ? *pb.at(at + e * BROWS) : T(0);
+            rc[e] = there ? *pc.at(at + e * BROWS) : T(0);
         }
     };
     // The piece of a sequence within the range, rows lo .. hi - 1, and in it the
@@ -320,9 +327,9 @@ __global__ __launch_bounds__(256, NS <= 4 ? 2 : 1) void gradient_kernel(const Ss
     };
     auto begin = [&](bool leaves) {
         if (JOINED && leaves)
-            load_states<NS>(a.heads + (r + 1) * dN + dn, nn, gr);
+            load_states<NS>(part_of(a.heads + (r + 1) * dN, dn), nn, gr);
         else
-            load_states<NS>(a.dstate_out + (a.dstate_out ? seg.seq * dN + dn : 0),
+            load_states<NS>(part_of(a.dstate_out + (a.dstate_out ? seg.seq * dN : 0), dn),
                             a.dstate_out ? nn : 0, gr);
     };
     enter(t1 - 1);
@@ -338,42 +345,50 @@ __global__ __launch_bounds__(256, NS <= 4 ? 2 : 1) void gradient_kernel(const Ss
             if (in.z)
                 rz.unpack(z);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float raw = d[i] + par[0][ch + i];
-                d[i] = in.softplus ? softplus(raw) : raw;
-                d[i] = row < n ? d[i] : 0.f;
-                if (in.z)
+            for (int i = 0; i < V; ++i)
+                d[i] += par[0][ch + i];
+            steps_of<V>(in.softplus, d);
+            if (row >= n) {  // rows past the step's last one change nothing
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    d[i] = u[i] = 0.f;
+            }
+            if (in.z) {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
                     e[i] *= silu(z[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
                 if (LANES_V * STEP >= 256 || row < STEP) {
                     dx[row][ch + i] = f2{d[i], d[i] * u[i]};
                     es[row][ch + i] = e[i];
                 }
             }
+            if (STEP * NP % 256 == 0 || br < STEP) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int i = tid + e * 256, br = i / NP, bn = i % NP;
-                if (STEP * NP % 256 == 0 || i < STEP * NP) {
-                    bc[br][bn / NS][bn % NS] = widen(rb[e]);
-                    bc[br][bn / NS][NS + bn % NS] = widen(rc[e]);
+                for (int e = 0; e < E; ++e) {
+                    bc[br + e * BROWS][bn / NS][bn % NS] = widen(rb[e]);
+                    bc[br + e * BROWS][bn / NS][NS + bn % NS] = widen(rc[e]);
                 }
             }
         }
         // the state before the step
         if (t == lo) {
             if (JOINED && seg.start < t0) {
-                load_states<NS>(a.ends + (r - 1) * dN + dn, nn, hs[0]);
+                load_states<NS>(part_of(a.ends + (r - 1) * dN, dn), nn, hs[0]);
             } else if (in.state_in) {
-                load_states<NS>(in.state_in + seg.seq * dN + dn, nn, hs[0]);
+                load_states<NS>(part_of(in.state_in + seg.seq * dN, dn), nn, hs[0]);
             } else {
                 zero_states(hs[0]);
             }
         } else {
             const int64_t m = t / STEP;
-            load_states<NS>(a.marks + m * dN + dn, nn, hs[0]);
+            load_states<NS>(part_of(a.marks + m * dN, dn), nn, hs[0]);
             if (JOINED && seg.start < t0) {
                 const float s = c < tile.left ? a.mark_sums[m * in.D + tile.d0 + c] : 0.f;
                 float h0[NS];
-                load_states<NS>(a.ends + (r - 1) * dN + dn, nn, h0);
+                load_states<NS>(part_of(a.ends + (r - 1) * dN, dn), nn, h0);
 #pragma unroll
                 for (int i = 0; i < NS; ++i)
                     hs[0][i] = fmaf(__builtin_amdgcn_exp2f(A2[i] * s), h0[i], hs[0][i]);
@@ -416,6 +431,7 @@ __global__ __launch_bounds__(256, NS <= 4 ? 2 : 1) void gradient_kernel(const Ss
             float sb[4], sa[4], sy[4];
 #pragma unroll
             for (int p0 = 4 - PER; p0 >= 0; p0 -= PER) {
+                __builtin_amdgcn_sched_barrier(0);
                 float v[LIVE];
 #pragma unroll
                 for (int p = PER - 1; p >= 0; --p) {
@@ -438,7 +454,9 @@ __global__ __launch_bounds__(256, NS <= 4 ? 2 : 1) void gradient_kernel(const Ss
                         const float qq = gr[i] * hs[kk][i];
                         sa[j] = fmaf(qq, A2[i], sa[j]);
                         dA[i] = fmaf(qq, x.x, dA[i]);
+                        pin(dA[i]);
                     }
+                    pin(sy[j]);
                 }
                 // over the 16 channels of the lane row
                 group_reduce<16, LIVE>(v, lane & 15);
@@ -459,13 +477,12 @@ __global__ __launch_bounds__(256, NS <= 4 ? 2 : 1) void gradient_kernel(const Ss
         }
         if (piece) {
             if (whole && a.out.dstate_in)
-                store_states<NS>(a.out.dstate_in + seq * dN + dn, nn, gr);
+                store_states<NS>(part_of(a.out.dstate_in + seq * dN, dn), nn, gr);
             if (more)
                 begin(false);
         }
         __syncthreads();
         if (row < rows) {
-            const int64_t k = at + row;
             float u[V], raw[V], du[V], dd[V];
             was_u.unpack(u);
             was_d.unpack(raw);
@@ -479,8 +496,8 @@ __global__ __launch_bounds__(256, NS <= 4 ? 2 : 1) void gradient_kernel(const Ss
                 sums[0][row][ch + i] = fmaf(e, u[i], sums[0][row][ch + i]);
                 sums[1][row][ch + i] += dd[i];
             }
-            store_some<V>((T *)a.out.du + k * a.out.ld_du + dv, left, du);
-            store_some<V>((T *)a.out.ddelta + k * a.out.ld_ddelta + dv, left, dd);
+            store_some<V>(Plane<T>(a.out.du, a.out.ld_du, row, dv).at(at), left, du);
+            store_some<V>(Plane<T>(a.out.ddelta, a.out.ld_ddelta, row, dv).at(at), left, dd);
             if (in.z) {
                 float e0[V], z[V], dz[V];
                 was_e.unpack(e0);
@@ -490,7 +507,7 @@ __global__ __launch_bounds__(256, NS <= 4 ? 2 : 1) void gradient_kernel(const Ss
                     const float y = fmaf(par[1][ch + i], u[i], oy[row][ch + i]);
                     dz[i] = e0[i] * y * silu_slope(z[i], sigmoid(z[i]));
                 }
-                store_some<V>((T *)a.out.dz + k * a.out.ld_dz + dv, left, dz);
+                store_some<V>(Plane<T>(a.out.dz, a.out.ld_dz, row, dv).at(at), left, dz);
             }
         }
         for (int i = tid; i < STEP * NP; i += 256) {
@@ -512,7 +529,7 @@ __global__ __launch_bounds__(256, NS <= 4 ? 2 : 1) void gradient_kernel(const Ss
         __syncthreads();  // es, ob, oa, oy and red are written again
     }
     float *part = a.part_par + r * (dN + 2 * in.D);
-    store_states<NS>(part + dn, nn, dA);
+    store_states<NS>(part_of(part, dn), nn, dA);
     __syncthreads();
     if (tid < 2 * kChannels && tid % kChannels < tile.left) {
         const int which = tid / kChannels, at = tid % kChannels;
@@ -583,9 +600,7 @@ template <typename T, int NS, bool JOINED> hipError_t walks(const SsmArgs &a, hi
         e = hipGetLastError();
     }
     if (JOINED && e == hipSuccess)
-        e = launch_carry(a, a.ends, a.sums, false, stream);
-    if (JOINED && e == hipSuccess)
-        e = launch_carry(a, a.heads, a.sums, true, stream);
+        e = launch_carry(a, stream);
     if (e != hipSuccess)
         return e;
     gradient_kernel<T, NS, JOINED><<<grid, 256, 0, stream>>>(a);
@@ -616,14 +631,13 @@ template <typename T> hipError_t backward(const SsmArgs &a, hipStream_t stream)
 
 }  // namespace
 
-// Workgroups wanted: two a CU run at once (registers), and two rounds of them
-// even out ranges of different work.
+// Joined ranges cost the first walk its sums for the gradients at their starts.
 SsmCut ssm_backward_cut(const lbi_ssm_inputs &in, bool ragged)
 {
-    return ssm_cut(in.T, in.sequences, in.D, in.G, ragged, 1024, ragged ? 32 : 64);
+    return ssm_cut(in.T, in.sequences, in.D, in.G, ragged, 0.15, 16);
 }
 
-int32_t ssm_backward_step(int32_t N) { return N <= 16 ? step_of(4) : (N <= 32 ? step_of(8) : step_of(16)); }
+int32_t ssm_backward_step(int32_t N) { return N <= 32 ? step_of(8) : step_of(16); }
 
 hipError_t launch_ssm_scan_backward(const SsmArgs &a, hipStream_t stream)
 {
