@@ -23,17 +23,19 @@ constexpr int kTile = 32;  // tokens staged at a time
 // Where it leaves the range, another workgroup may already have written its new
 // state (state_out may be state_in), so the first walk's copy is read.
 template <int NS>
-__device__ __forceinline__ void begin_states(const SsmArgs &a, const Segment &seg, int64_t r,
-                                             int64_t t1, uint32_t dn, int nn, float (&h)[NS])
+__device__ __forceinline__ void begin_states(const Segment &seg, int64_t r, int64_t t1,
+                                             uint32_t dn, int nn, float (&h)[NS])
 {
-    const int64_t dN = (int64_t)a.in.D * a.in.N;
-    if (!a.in.state_in) {
+    const PassedArgs p = passed();
+    const int64_t dN = (int64_t)p->in.D * p->in.N;
+    if (!p->in.state_in) {
         zero_states(h);
-    } else if (a.cut.joined && seg.end > t1) {
-        load_states<NS>(part_of(a.starts + r * dN, dn), nn, h);
+    } else if (p->cut.joined && seg.end > t1) {
+        load_states<NS>(part_of(p->starts + r * dN, dn), nn, h);
     } else {
-        const int64_t row = state_row(a.slots, a.n_slots, seg.seq);
-        load_states<NS>(part_of(a.in.state_in + (row < 0 ? 0 : row) * dN, dn), row < 0 ? 0 : nn, h);
+        const int64_t row = state_row(p->slots, p->n_slots, seg.seq);
+        load_states<NS>(part_of(p->in.state_in + (row < 0 ? 0 : row) * dN, dn), row < 0 ? 0 : nn,
+                        h);
     }
 }
 
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(256, NS <= 4 ? 4 : 2) void scan_kernel(const SsmArg
         if (seg.start < t0)
             load_states<NS>(part_of(a.ends + (r - 1) * dN, dn), nn, h);
         else
-            begin_states<NS>(a, seg, r, t1, dn, nn, h);
+            begin_states<NS>(seg, r, t1, dn, nn, h);
     }
     float A2[NS];
     load_states<NS>(part_of(in.A, dn), nn, A2);
@@ -116,21 +118,21 @@ __global__ __launch_bounds__(256, NS <= 4 ? 4 : 2) void scan_kernel(const SsmArg
     Raw<T, 8> ru, rd, rz;
     T rb[E], rc[E];
     const int br = tid / NP, bn = tid % NP, bcol = tile.group * in.N + bn;
-    const Plane<T> pu(in.u, in.ld_u, row, d8), pd(in.delta, in.ld_delta, row, d8),
-        pz(in.z, in.ld_z, row, d8), py(a.y, a.ld_y, row, d8), pb(in.B, in.ld_B, br, bcol),
-        pc(in.C, in.ld_C, br, bcol);
+    const Plane<T> pu(in.ld_u, row, d8), pd(in.ld_delta, row, d8), pz(in.ld_z, row, d8),
+        py(a.ld_y, row, d8), pb(in.ld_B, br, bcol), pc(in.ld_C, br, bcol);
     auto load = [&](int64_t at, int n) {
         const int m = row < n ? left : 0;
-        ru.load(pu.at(at), m);
-        rd.load(pd.at(at), m);
-        if (!ENDS && in.z)
-            rz.load(pz.at(at), m);
+        const SsmArgs *const p = &a;
+        ru.load(pu.at(p->in.u, p->in.ld_u, at), m);
+        rd.load(pd.at(p->in.delta, p->in.ld_delta, at), m);
+        if (!ENDS && p->in.z)
+            rz.load(pz.at(p->in.z, p->in.ld_z, at), m);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const bool there = br + e * BROWS < n && bn < in.N;
-            rb[e] = there ? *pb.at(at + e * BROWS) : T(0);
+            const bool there = br + e * BROWS < n && bn < p->in.N;
+            rb[e] = there ? *pb.at(p->in.B, p->in.ld_B, at + e * BROWS) : T(0);
             if (!ENDS)
-                rc[e] = there ? *pc.at(at + e * BROWS) : T(0);
+                rc[e] = there ? *pc.at(p->in.C, p->in.ld_C, at + e * BROWS) : T(0);
         }
     };
     auto tile_rows = [&](const Segment &s, int64_t at) {
@@ -208,13 +210,14 @@ __global__ __launch_bounds__(256, NS <= 4 ? 4 : 2) void scan_kernel(const SsmArg
             }
         }
         if (!ENDS && ended) {
-            if (a.state_out) {
-                const int64_t to = state_row(a.slots, a.n_slots, was.seq);
+            const PassedArgs p = passed();
+            if (p->state_out) {
+                const int64_t to = state_row(p->slots, p->n_slots, was.seq);
                 if (to >= 0)
-                    store_states<NS>(part_of(a.state_out + to * dN, dn), nn, h);
+                    store_states<NS>(part_of(p->state_out + to * p->in.D * p->in.N, dn), nn, h);
             }
             if (more)
-                begin_states<NS>(a, seg, r, t1, dn, nn, h);
+                begin_states<NS>(seg, r, t1, dn, nn, h);
         }
         __syncthreads();
         if (!ENDS && row < rows) {
@@ -228,7 +231,7 @@ __global__ __launch_bounds__(256, NS <= 4 ? 4 : 2) void scan_kernel(const SsmArg
                 for (int i = 0; i < 8; ++i)
                     y[i] *= silu(zz[i]);
             }
-            store_some<8>(py.at(at), left, y);
+            store_some<8>(py.at(a.y, a.ld_y, at), left, y);
         }
         if (!more)
             break;

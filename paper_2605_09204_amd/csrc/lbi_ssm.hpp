@@ -51,20 +51,29 @@ template <typename T> __device__ __forceinline__ T *lane_address(T *uniform, uin
 // that nothing reads until a walk's end past the walk, and keep their terms).
 __device__ __forceinline__ void pin(float &x) { asm volatile("" : "+v"(x)); }
 
-// A token tensor as a staging thread sees it: the rows of a tile begin at a uniform
-// address, its own part of them at a 32-bit offset from there (row strides are
-// limited to that end).
+// The kernel's own arguments, read again from where they were passed: within a loop
+// over tiles, so that some fifty pointers and strides are not held in scalar
+// registers (of which there are 102; the compiler spilled them to lanes of vector
+// registers, and an eighth of the gradient kernel's instructions fetched them back).
+typedef const __attribute__((address_space(4))) SsmArgs *PassedArgs;
+__device__ __forceinline__ PassedArgs passed()
+{
+    PassedArgs p = (PassedArgs)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return p;
+}
+
+// A staging thread's part of a tile's rows in a token tensor, as a 32-bit offset
+// from the uniform address of the first row (row strides are limited to that end).
 template <typename T> struct Plane {
-    T *base;
-    int64_t ld;
     uint32_t offset;  // bytes
-    __device__ __forceinline__ Plane(const void *p, int64_t stride, int row, int col)
-        : base((T *)p), ld(stride), offset((uint32_t)((row * (int)stride + col) * (int)sizeof(T)))
+    __device__ __forceinline__ Plane(int64_t ld, int row, int col)
+        : offset((uint32_t)((row * (int)ld + col) * (int)sizeof(T)))
     {
     }
-    __device__ __forceinline__ T *at(int64_t t) const
+    __device__ __forceinline__ T *at(const void *base, int64_t ld, int64_t t) const
     {
-        return lane_address(base + t * ld, offset);
+        return lane_address((T *)base + t * ld, offset);
     }
 };
 // The same for arrays [.][D][N] of states: `bytes` is the thread's own part.
@@ -141,6 +150,20 @@ __device__ __forceinline__ void store_states(float *p, int n, const float (&h)[N
                 p[i] = h[i];
     }
 }
+// V values of LDS, at an address aligned to them (16 bytes at most).
+template <int V> __device__ __forceinline__ void read_lds(const float *p, float (&v)[V])
+{
+    if constexpr (V == 2) {
+        const f2 q = *(const f2 *)p;
+        v[0] = q.x; v[1] = q.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const f4 q = *(const f4 *)(p + i);
+            v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
+        }
+    }
+}
 template <int NS> __device__ __forceinline__ void zero_states(float (&h)[NS])
 {
 #pragma unroll
@@ -162,51 +185,68 @@ __device__ __forceinline__ float sum_states(const float (&v)[4])
 // the ranges that follow each other: one thread a channel and state.  A thread has
 // the ends of DEEP ranges in flight: its time is that many fewer trips to memory.
 template <int DEEP>
-__global__ __launch_bounds__(256) void carry_kernel(const SsmArgs a)
+__global__ __launch_bounds__(64) void carry_kernel(const SsmArgs a)
 {
     const int64_t dN = (int64_t)a.in.D * a.in.N;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= dN)
-        return;
+    int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x;
+    const bool live = i < dN;
+    if (!live)
+        i = dN - 1;  // such lanes only help with the flags
     const bool reverse = blockIdx.z == 1;
     const int64_t d = i / a.in.N;
     const int64_t count = a.cut.per_sequence > 0 ? a.cut.per_sequence : a.cut.ranges;
     const int64_t first = (int64_t)blockIdx.y * count;
     const int32_t stops = reverse ? kEnds : kStarts;
-    float *ends = reverse ? a.heads : a.ends;
     const float A2 = a.in.A[i] * kLog2e;
+    const int64_t from = reverse ? first + count - 1 : first, one = reverse ? -1 : 1;
+    const int64_t down = one * dN, along = one * a.in.D;  // to the next range
+    float *ends = (reverse ? a.heads : a.ends) + from * dN + i;
+    const float *sums = a.sums + from * a.in.D + d;
+    const int32_t *flags = a.flags + from;
     float cur = 0.f;
-    for (int64_t k = 0; k < count; k += DEEP) {
+    auto batch = [&](auto whole, int rest) {
+        constexpr bool WHOLE = decltype(whole)::value;  // DEEP ranges, else `rest`
+        const int lane = threadIdx.x;
+        const uint64_t stop = __ballot(lane < rest && (flags[lane < rest ? lane * one : 0] & stops));
         float e[DEEP], w[DEEP];
-        int32_t f[DEEP];
+        float *p = ends;
+        const float *s = sums;
 #pragma unroll
         for (int j = 0; j < DEEP; ++j) {
-            // (past the last range the last one again: nothing is stored then)
-            const int64_t at = k + j < count ? k + j : count - 1;
-            const int64_t r = first + (reverse ? count - 1 - at : at);
-            e[j] = ends[r * dN + i];
-            w[j] = a.sums[r * a.in.D + d];
-            f[j] = a.flags[r];
-        }
-#pragma unroll
-        for (int j = 0; j < DEEP; ++j) {
-            if (k + j < count) {
-                const int64_t r = first + (reverse ? count - 1 - (k + j) : k + j);
-                cur = f[j] & stops ? e[j] : fmaf(__builtin_amdgcn_exp2f(A2 * w[j]), cur, e[j]);
-                ends[r * dN + i] = cur;
+            if (WHOLE || j < rest) {
+                e[j] = *p;
+                w[j] = *s;
+                p += down;
+                s += along;
             }
         }
-    }
+#pragma unroll
+        for (int j = 0; j < DEEP; ++j) {
+            if (WHOLE || j < rest) {
+                cur = stop >> j & 1 ? e[j] : fmaf(__builtin_amdgcn_exp2f(A2 * w[j]), cur, e[j]);
+                if (live)
+                    *ends = cur;
+                ends += down;
+            }
+        }
+        sums = s;
+        flags += rest * one;
+    };
+    int64_t k = 0;
+    for (; k + DEEP <= count; k += DEEP)
+        batch(std::true_type{}, DEEP);
+    if (k < count)
+        batch(std::false_type{}, (int)(count - k));
 }
 inline hipError_t launch_carry(const SsmArgs &a, hipStream_t stream)
 {
     const int64_t dN = (int64_t)a.in.D * a.in.N;
     const int64_t chains = a.cut.per_sequence > 0 ? a.cut.ranges / a.cut.per_sequence : 1;
-    const dim3 grid((unsigned)((dN + 255) / 256), (unsigned)chains, a.heads ? 2 : 1);
+    const dim3 grid((unsigned)((dN + 63) / 64), (unsigned)chains, a.heads ? 2 : 1);
     if (a.cut.ranges / chains <= 8)
-        carry_kernel<8><<<grid, 256, 0, stream>>>(a);
+        carry_kernel<8><<<grid, 64, 0, stream>>>(a);
     else
-        carry_kernel<32><<<grid, 256, 0, stream>>>(a);
+        carry_kernel<32><<<grid, 64, 0, stream>>>(a);
     return hipGetLastError();
 }
 

@@ -89,24 +89,24 @@ __global__ __launch_bounds__(256, NS <= 2 ? 4 : (NS == 4 ? 3 : (NS == 8 ? 2 : 1)
     Raw<T, 8> ru, rd, rz, re;
     T rb[E], rc[E];
     const int br = tid / NP, bn = tid % NP, bcol = tile.group * in.N + bn;
-    const Plane<T> pu(in.u, in.ld_u, row, d8), pd(in.delta, in.ld_delta, row, d8),
-        pz(in.z, in.ld_z, row, d8), pe(a.dy, a.ld_dy, row, d8), pb(in.B, in.ld_B, br, bcol),
-        pc(in.C, in.ld_C, br, bcol);
+    const Plane<T> pu(in.ld_u, row, d8), pd(in.ld_delta, row, d8), pz(in.ld_z, row, d8),
+        pe(a.ld_dy, row, d8), pb(in.ld_B, br, bcol), pc(in.ld_C, br, bcol);
     auto load = [&](int64_t at, int n, bool heads) {
         const int m = row < n ? left : 0;
-        ru.load(pu.at(at), m);
-        rd.load(pd.at(at), m);
+        const SsmArgs *const p = &a;
+        ru.load(pu.at(p->in.u, p->in.ld_u, at), m);
+        rd.load(pd.at(p->in.delta, p->in.ld_delta, at), m);
         if (JOINED && heads) {
-            re.load(pe.at(at), m);
-            if (in.z)
-                rz.load(pz.at(at), m);
+            re.load(pe.at(p->dy, p->ld_dy, at), m);
+            if (p->in.z)
+                rz.load(pz.at(p->in.z, p->in.ld_z, at), m);
         }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const bool there = br + e * BROWS < n && bn < in.N;
-            rb[e] = there ? *pb.at(at + e * BROWS) : T(0);
+            const bool there = br + e * BROWS < n && bn < p->in.N;
+            rb[e] = there ? *pb.at(p->in.B, p->in.ld_B, at + e * BROWS) : T(0);
             if (JOINED && heads)
-                rc[e] = there ? *pc.at(at + e * BROWS) : T(0);
+                rc[e] = there ? *pc.at(p->in.C, p->in.ld_C, at + e * BROWS) : T(0);
         }
     };
     auto tile_rows = [&](int64_t at) {
@@ -231,9 +231,13 @@ __global__ __launch_bounds__(256, NS <= 2 ? 4 : (NS == 4 ? 3 : (NS == 8 ? 2 : 1)
     }
 }
 
-// The second walk.
+// The second walk.  Wavefronts a SIMD: as many as its registers allow.
+template <typename T> constexpr int waves_of(int NS)
+{
+    return NS <= 4 && sizeof(T) == 2 ? 3 : (NS <= 8 ? 2 : 1);
+}
 template <typename T, int NS, bool JOINED>
-__global__ __launch_bounds__(256, NS <= 4 ? 3 : 2) void gradient_kernel(const SsmArgs a)
+__global__ __launch_bounds__(256, waves_of<T>(NS)) void gradient_kernel(const SsmArgs a)
 {
     constexpr int STEP = step_of(NS), NP = 4 * NS;
     constexpr int V = STEP <= 8 ? 2 : 4;             // channels a thread stages
@@ -296,21 +300,21 @@ __global__ __launch_bounds__(256, NS <= 4 ? 3 : 2) void gradient_kernel(const Ss
     Raw<T, V> ru, rd, rz, re;
     T rb[E], rc[E];
     const int br = tid / NP, bn = tid % NP, bcol = tile.group * in.N + bn;
-    const Plane<T> pu(in.u, in.ld_u, row, dv), pd(in.delta, in.ld_delta, row, dv),
-        pz(in.z, in.ld_z, row, dv), pe(a.dy, a.ld_dy, row, dv), pb(in.B, in.ld_B, br, bcol),
-        pc(in.C, in.ld_C, br, bcol);
+    const Plane<T> pu(in.ld_u, row, dv), pd(in.ld_delta, row, dv), pz(in.ld_z, row, dv),
+        pe(a.ld_dy, row, dv), pb(in.ld_B, br, bcol), pc(in.ld_C, br, bcol);
     auto load = [&](int64_t at, int n) {
         const int m = row < n ? left : 0;
-        ru.load(pu.at(at), m);
-        rd.load(pd.at(at), m);
-        re.load(pe.at(at), m);
-        if (in.z)
-            rz.load(pz.at(at), m);
+        const PassedArgs p = passed();
+        ru.load(pu.at(p->in.u, p->in.ld_u, at), m);
+        rd.load(pd.at(p->in.delta, p->in.ld_delta, at), m);
+        re.load(pe.at(p->dy, p->ld_dy, at), m);
+        if (p->in.z)
+            rz.load(pz.at(p->in.z, p->in.ld_z, at), m);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const bool there = br + e * BROWS < n && bn < in.N;
-            rb[e] = there ? *pb.at(at + e * BROWS) : T(0);
-            rc[e] = there ? *pc.at(at + e * BROWS) : T(0);
+            const bool there = br + e * BROWS < n && bn < p->in.N;
+            rb[e] = there ? *pb.at(p->in.B, p->in.ld_B, at + e * BROWS) : T(0);
+            rc[e] = there ? *pc.at(p->in.C, p->in.ld_C, at + e * BROWS) : T(0);
         }
     };
     // The piece of a sequence within the range, rows lo .. hi - 1, and in it the
@@ -326,15 +330,45 @@ __global__ __launch_bounds__(256, NS <= 4 ? 3 : 2) void gradient_kernel(const Ss
         n = (int)(hi - t);
     };
     auto begin = [&](bool leaves) {
+        const PassedArgs p = passed();
+        const int64_t dN = (int64_t)p->in.D * p->in.N;
         if (JOINED && leaves)
-            load_states<NS>(part_of(a.heads + (r + 1) * dN, dn), nn, gr);
+            load_states<NS>(part_of(p->heads + (r + 1) * dN, dn), nn, gr);
         else
-            load_states<NS>(part_of(a.dstate_out + (a.dstate_out ? seg.seq * dN : 0), dn),
-                            a.dstate_out ? nn : 0, gr);
+            load_states<NS>(part_of(p->dstate_out + (p->dstate_out ? seg.seq * dN : 0), dn),
+                            p->dstate_out ? nn : 0, gr);
+    };
+    // The state before the step at t, loaded ahead of its use: the piece's first
+    // state, or a mark, which is completed by the state that entered the range.
+    float next_h[NS], next_sum = 0.f, entry[NS];
+    bool has_entry = false;
+    zero_states(entry);
+    auto load_state = [&]() {
+        const PassedArgs p = passed();
+        const int64_t dN = (int64_t)p->in.D * p->in.N;
+        if (JOINED && seg.start < t0 && !has_entry) {
+            load_states<NS>(part_of(p->ends + (r - 1) * dN, dn), nn, entry);
+            has_entry = true;
+        }
+        if (t > lo) {
+            const int64_t m = t / STEP;
+            load_states<NS>(part_of(p->marks + m * dN, dn), nn, next_h);
+            if (JOINED && seg.start < t0)
+                next_sum = c < tile.left ? p->mark_sums[m * p->in.D + tile.d0 + c] : 0.f;
+        } else if (JOINED && seg.start < t0) {
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+                next_h[i] = entry[i];
+        } else if (p->in.state_in) {
+            load_states<NS>(part_of(p->in.state_in + seg.seq * dN, dn), nn, next_h);
+        } else {
+            zero_states(next_h);
+        }
     };
     enter(t1 - 1);
     begin(seg.end > t1);
     load(t, n);
+    load_state();
     while (true) {
         const Raw<T, V> was_u = ru, was_d = rd, was_e = re, was_z = rz;
         {
@@ -374,25 +408,13 @@ __global__ __launch_bounds__(256, NS <= 4 ? 3 : 2) void gradient_kernel(const Ss
             }
         }
         // the state before the step
-        if (t == lo) {
-            if (JOINED && seg.start < t0) {
-                load_states<NS>(part_of(a.ends + (r - 1) * dN, dn), nn, hs[0]);
-            } else if (in.state_in) {
-                load_states<NS>(part_of(in.state_in + seg.seq * dN, dn), nn, hs[0]);
-            } else {
-                zero_states(hs[0]);
-            }
-        } else {
-            const int64_t m = t / STEP;
-            load_states<NS>(part_of(a.marks + m * dN, dn), nn, hs[0]);
-            if (JOINED && seg.start < t0) {
-                const float s = c < tile.left ? a.mark_sums[m * in.D + tile.d0 + c] : 0.f;
-                float h0[NS];
-                load_states<NS>(part_of(a.ends + (r - 1) * dN, dn), nn, h0);
 #pragma unroll
-                for (int i = 0; i < NS; ++i)
-                    hs[0][i] = fmaf(__builtin_amdgcn_exp2f(A2[i] * s), h0[i], hs[0][i]);
-            }
+        for (int i = 0; i < NS; ++i)
+            hs[0][i] = next_h[i];
+        if (JOINED && seg.start < t0 && t > lo) {
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+                hs[0][i] = fmaf(__builtin_amdgcn_exp2f(A2[i] * next_sum), entry[i], hs[0][i]);
         }
         __syncthreads();
         const int64_t at = t, from = lo, seq = seg.seq;
@@ -407,6 +429,7 @@ __global__ __launch_bounds__(256, NS <= 4 ? 3 : 2) void gradient_kernel(const Ss
                 n = STEP;
             }
             load(t, n);
+            load_state();
         }
         float w[KEEP ? STEP : 1][NS];
 #pragma unroll
@@ -438,10 +461,12 @@ __global__ __launch_bounds__(256, NS <= 4 ? 3 : 2) void gradient_kernel(const Ss
                     const int j = p0 + p, kk = k + j;
                     const f2 x = dx[kk][c2];
                     const float e = es[kk][c2];
+                    float bcs[2 * NS];
+                    read_lds<2 * NS>(bc[kk][g2], bcs);
                     sb[j] = sa[j] = sy[j] = 0.f;
 #pragma unroll
                     for (int i = 0; i < NS; ++i) {
-                        const float b = bc[kk][g2][i], cc = bc[kk][g2][NS + i];
+                        const float b = bcs[i], cc = bcs[NS + i];
                         float dec;
                         if constexpr (KEEP) dec = w[kk][i];
                         else dec = __builtin_amdgcn_exp2f(x.x * A2[i]);
@@ -476,8 +501,9 @@ __global__ __launch_bounds__(256, NS <= 4 ? 3 : 2) void gradient_kernel(const Ss
                 oy[k + g][c] = sum_states(sy);
         }
         if (piece) {
-            if (whole && a.out.dstate_in)
-                store_states<NS>(part_of(a.out.dstate_in + seq * dN, dn), nn, gr);
+            const PassedArgs p = passed();
+            if (whole && p->out.dstate_in)
+                store_states<NS>(part_of(p->out.dstate_in + seq * p->in.D * p->in.N, dn), nn, gr);
             if (more)
                 begin(false);
         }
@@ -496,8 +522,10 @@ __global__ __launch_bounds__(256, NS <= 4 ? 3 : 2) void gradient_kernel(const Ss
                 sums[0][row][ch + i] = fmaf(e, u[i], sums[0][row][ch + i]);
                 sums[1][row][ch + i] += dd[i];
             }
-            store_some<V>(Plane<T>(a.out.du, a.out.ld_du, row, dv).at(at), left, du);
-            store_some<V>(Plane<T>(a.out.ddelta, a.out.ld_ddelta, row, dv).at(at), left, dd);
+            const PassedArgs p = passed();
+            store_some<V>(Plane<T>(p->out.ld_du, row, dv).at(p->out.du, p->out.ld_du, at), left, du);
+            store_some<V>(Plane<T>(p->out.ld_ddelta, row, dv)
+                             .at(p->out.ddelta, p->out.ld_ddelta, at), left, dd);
             if (in.z) {
                 float e0[V], z[V], dz[V];
                 was_e.unpack(e0);
@@ -507,12 +535,14 @@ __global__ __launch_bounds__(256, NS <= 4 ? 3 : 2) void gradient_kernel(const Ss
                     const float y = fmaf(par[1][ch + i], u[i], oy[row][ch + i]);
                     dz[i] = e0[i] * y * silu_slope(z[i], sigmoid(z[i]));
                 }
-                store_some<V>(Plane<T>(a.out.dz, a.out.ld_dz, row, dv).at(at), left, dz);
+                store_some<V>(Plane<T>(p->out.ld_dz, row, dv).at(p->out.dz, p->out.ld_dz, at), left,
+                             dz);
             }
         }
         for (int i = tid; i < STEP * NP; i += 256) {
+            const PassedArgs p = passed();
             const int br = i / NP, bn = i % NP;
-            if (br < rows && bn < in.N) {
+            if (br < rows && bn < p->in.N) {
                 f2 s = *(const f2 *)red[0][br][bn];
 #pragma unroll
                 for (int x = 1; x < 4; ++x) {
@@ -520,13 +550,15 @@ __global__ __launch_bounds__(256, NS <= 4 ? 3 : 2) void gradient_kernel(const Ss
                     s.x += o.x;
                     s.y += o.y;
                 }
-                const int64_t o = (((int64_t)tile.tile * in.T + at + br) * in.G + tile.group) * in.N;
-                *(f2 *)(a.part_bc + (o + bn) * 2) = s;
+                const int64_t row0 = (int64_t)tile.tile * p->in.T + at, gn = p->in.G * p->in.N;
+                *(f2 *)lane_address(p->part_bc + row0 * gn * 2,
+                                    (uint32_t)(br * (int)gn + tile.group * p->in.N + bn) * 8u) = s;
             }
         }
         if (!more)
             break;
-        __syncthreads();  // es, ob, oa, oy and red are written again
+        // No barrier: what the threads write before the next one are entries of
+        // dx and es that only they themselves read here, and bc, that none does.
     }
     float *part = a.part_par + r * (dN + 2 * in.D);
     store_states<NS>(part_of(part, dn), nn, dA);
