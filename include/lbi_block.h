@@ -54,7 +54,7 @@ extern "C" {
 #define LBI_NORM_MAX_D 16384 /* longest row of the norm                        */
 #define LBI_SSM_MAX_D 65536  /* most channels of the convolution and the scan  */
 #define LBI_SSM_MAX_N 64     /* most states of a channel                       */
-#define LBI_SSM_MAX_LD (1 << 23) /* longest row stride of the scan's tensors   */
+#define LBI_SSM_MAX_LD (1 << 23) /* longest row stride of their token tensors  */
 #define LBI_CONV_MAX_W 4     /* most taps of the convolution                   */
 
 /* Formats of an 8-bit output. */

@@ -227,6 +227,23 @@ struct Sequences {
         }
         return lo;
     }
+    // The same by a whole wavefront with one t: 64 offsets at a time, so one or two
+    // trips to memory instead of one a halving.
+    __device__ __forceinline__ int64_t find_together(int64_t t) const
+    {
+        if (!offsets)
+            return len > 0 ? t / len : 0;
+        const int lane = threadIdx.x & 63;
+        int64_t lo = 0, n = B;  // among lo .. lo + n - 1
+        while (n > 1) {
+            const int64_t step = (n + 63) / 64, i = lo + lane * step;
+            const int before = __popcll(__ballot(lane * step < n && at(i) <= t));
+            const int64_t skip = before > 0 ? (before - 1) * step : 0;
+            lo += skip;
+            n = n - skip < step ? n - skip : step;
+        }
+        return lo;
+    }
     // The next sequence after i that is not empty, or B.
     __device__ __forceinline__ int64_t next(int64_t i) const
     {
@@ -240,9 +257,10 @@ struct Sequences {
 struct Segment {
     int64_t seq, start, end;
 
-    __device__ __forceinline__ void enter(const Sequences &q, int64_t t)
+    // together: by all lanes of a wavefront, with the same t
+    __device__ __forceinline__ void enter(const Sequences &q, int64_t t, bool together)
     {
-        seq = q.find(t);
+        seq = together ? q.find_together(t) : q.find(t);
         start = q.at(seq);
         end = q.at(seq + 1);
         if (start > t) start = t;  // only with offsets that do not ascend

@@ -172,7 +172,7 @@ struct ScanTensors {
     }
 };
 
-// A tile's rows are addressed by 32-bit offsets in bytes.
+// The rows of a tile or piece are addressed by 32-bit distances in bytes.
 bool too_wide(std::initializer_list<int64_t> strides)
 {
     for (int64_t ld : strides)
@@ -313,7 +313,8 @@ lbi_status lbi_ssm_conv(const void *x, int64_t ld_x, const float *weight, const 
 {
     if (!known(dt))
         return LBI_ERR_DTYPE;
-    if (bad_conv_shape(T, B, D, W, offsets != nullptr) || (slots && n_slots < 0))
+    if (bad_conv_shape(T, B, D, W, offsets != nullptr) || (slots && n_slots < 0) ||
+        too_wide({ld_x, ld_out}))
         return LBI_ERR_SHAPE;
     if (B == 0)
         return LBI_OK;
@@ -357,7 +358,7 @@ lbi_status lbi_ssm_conv_backward(const void *x, int64_t ld_x, const float *weigh
 {
     if (!known(dt))
         return LBI_ERR_DTYPE;
-    if (bad_conv_shape(T, B, D, W, offsets != nullptr))
+    if (bad_conv_shape(T, B, D, W, offsets != nullptr) || too_wide({ld_x, ld_dout, ld_dx}))
         return LBI_ERR_SHAPE;
     if (!weight || !dweight || (T > 0 && (!x || !dout || !dx)))
         return LBI_ERR_NULL;

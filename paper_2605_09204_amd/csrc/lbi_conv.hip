@@ -1,20 +1,21 @@
 // Short causal convolution along packed sequences, channel by channel: forward,
 // gradient, and one token a sequence.
 //
-// A thread owns a few consecutive channels and walks a run of tokens with the
-// last W - 1 of them in registers, so every value is loaded once a run (and
-// the W - 1 tokens before the run once more, from cache).  The bytes are the
-// tensors' own, a few operations for each: the bound is HBM.  Lanes of a
-// workgroup lie along the channels (one row's values are contiguous) and, above
-// that, along the runs; the length of a run is chosen so that about 2^17
-// threads exist, which is what keeps enough loads in flight.
+// A thread owns V consecutive channels and a run of tokens, which it takes in pieces
+// of up to PIECE tokens of one sequence.  All rows of a piece and the W - 1 before it
+// are loaded at once, so that some twenty loads of a thread are in flight, and
+// everything else happens in registers.  The bytes are the tensors' own (the rows
+// around a piece come from cache), a few operations for each: the bound is HBM.
+// Lanes of a workgroup lie along the channels (a row's values are contiguous) and,
+// above that, along the runs.
 #include "lbi_block.hpp"
 
 namespace lbi {
 namespace {
 
-constexpr int64_t kThreads = 1 << 17;  // threads wanted in all
-constexpr int kBatch = 4;              // tokens loaded ahead of their use
+constexpr int64_t kThreads = 1 << 17;  // threads wanted in all: eight wavefronts a CU
+constexpr int kPiece = 8;
+template <typename T> constexpr int backward_piece_rows() { return 32 / sizeof(T); }
 
 // How a [tokens][channels] plane is cut: lanes along the channels (a power of
 // two), runs beside them in a workgroup of 256, and tokens a run.
@@ -35,10 +36,58 @@ Cut cut_of(int64_t T, int32_t D, int V, int most_lanes, int least, int most)
     const int64_t per = (int64_t)runs * tokens;
     return {lanes, runs, tokens, (T + per - 1) / per, (vec + lanes - 1) / lanes};
 }
-// Forward: 8 channels a lane, gradient: 4 (its sums and its tokens in flight
-// take twice the registers).
-Cut forward_cut(int64_t T, int32_t D) { return cut_of(T, D, 8, 32, 4, 64); }
-Cut backward_cut(int64_t T, int32_t D) { return cut_of(T, D, 4, 64, 8, 256); }
+// Forward: 16 bytes a lane.  Gradient: 4 channels a lane (its sums and its rows in
+// flight take twice the registers), and longer runs, which leave fewer partial sums.
+int forward_width(bool bf16) { return bf16 ? 8 : 4; }
+Cut forward_cut(int64_t T, int32_t D, bool bf16)
+{
+    return cut_of(T, D, forward_width(bf16), 64, 4, kPiece);
+}
+Cut backward_cut(int64_t T, int32_t D) { return cut_of(T, D, 4, 64, 4, 512); }
+
+// The last vector of a row whose width is no multiple of V moves back to end with
+// the row: some channels are then computed twice, to the same values, and no lane
+// works on a part of a vector (unless the row is shorter than one).
+template <int V> __device__ __forceinline__ void whole_vector(int32_t D, int *d, int *left)
+{
+    if (*left < V && D >= V) {
+        *d = D - V;
+        *left = V;
+    }
+}
+
+// Row i of the rows from p on, or the last one that is there: a load that no lane has
+// to skip.  (Row strides are limited, so the distance fits 32 bits.)
+template <typename T>
+__device__ __forceinline__ const T *row_at(const T *p, int i, int there, uint32_t bytes)
+{
+    return (const T *)((const char *)p + (uint64_t)(uint32_t)(i < there ? i : there) * bytes);
+}
+
+// V values of a row: all of them (FULL), or the first `left`.
+template <bool FULL, int V, typename T>
+__device__ __forceinline__ void load_row(const T *p, int left, Raw<T, V> &r)
+{
+    if constexpr (FULL) {
+        r.load(p, V);
+    } else {
+        // a loop that stays one: this is the last lane of a row whose width is no
+        // multiple of V
+        T v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            v[i] = p[i < left ? i : 0];
+        __builtin_memcpy(&r, v, sizeof(r));
+    }
+}
+template <bool FULL, int V, typename T>
+__device__ __forceinline__ void store_row(T *p, int left, const float (&v)[V])
+{
+    if constexpr (FULL)
+        store_all<V>(p, v);
+    else
+        store_some<V>(p, left, v);
+}
 
 // The taps of V channels, weight[d][w] -> k[w][i].
 template <int W, int V>
@@ -51,31 +100,41 @@ __device__ __forceinline__ void load_taps(const float *weight, int d, int left, 
             k[w][i] = i < left ? weight[(int64_t)(d + i) * W + w] : 0.f;
 }
 
-// The W - 1 tokens before row t of a sequence, oldest first: rows of x, or of
-// the state where the sequence has not that many.
+// The W - 1 rows of x before row t, oldest first, ahead of knowing whose they are...
 template <int W, int V, typename T>
-__device__ __forceinline__ void load_window(const ConvArgs &a, const Segment &seg, int64_t t, int d,
-                                            int left, float (&win)[W - 1][V])
+__device__ __forceinline__ void load_rows_before(const ConvArgs &a, int64_t t, int d, int left,
+                                                 Raw<T, V> (&before)[W - 1])
 {
-    const int64_t slot = a.state_in ? state_row(a.slots, a.n_slots, seg.seq) : -1;
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
         const int64_t row = t - (W - 1) + j;
-        if (row >= seg.start) {
-            load_some<V>((const T *)a.x + row * a.ld_x + d, left, win[j]);
-        } else if (slot >= 0) {
-            const int64_t k = (W - 1) + (row - seg.start);
-            load_some<V>((const T *)a.state_in + (slot * (W - 1) + k) * a.D + d, left, win[j]);
-        } else {
+        before[j].load((const T *)a.x + d + (row > 0 ? row : 0) * a.ld_x, left);
+    }
+}
+// ... and the W - 1 tokens before row t of its sequence: these, or rows of the state
+// where the sequence has not that many.
+template <int W, int V, typename T>
+__device__ __forceinline__ void window_of(const ConvArgs &a, const Segment &seg, int64_t t, int d,
+                                          int left, const Raw<T, V> (&before)[W - 1],
+                                          float (&win)[W - 1][V])
+{
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                win[j][i] = 0.f;
-        }
+    for (int j = 0; j < W - 1; ++j)
+        before[j].unpack(win[j]);
+    if (t - seg.start >= W - 1)
+        return;
+    const int64_t slot = a.state_in ? state_row(a.slots, a.n_slots, seg.seq) : -1;
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+        const int64_t row = t - (W - 1) + j, k = (W - 1) + (row - seg.start);
+        if (row < seg.start)
+            load_some<V>((const T *)a.state_in + (slot < 0 ? 0 : (slot * (W - 1) + k) * a.D + d),
+                         slot < 0 ? 0 : left, win[j]);
     }
 }
 
 // The state after sequence s: the last W - 1 of its old state and its tokens.
-template <int W, typename T>
+template <int W, int V, typename T>
 __device__ __forceinline__ void write_state(const ConvArgs &a, const Sequences &q, int64_t s, int d,
                                             int left)
 {
@@ -83,30 +142,88 @@ __device__ __forceinline__ void write_state(const ConvArgs &a, const Sequences &
     if (slot < 0)
         return;
     const int64_t start = q.at(s), len = q.at(s + 1) - start;
-    float v[W - 1][8];
+    float v[W - 1][V];
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
         const int64_t p = len - (W - 1) + j;
         if (p >= 0)
-            load_some<8>((const T *)a.x + (start + p) * a.ld_x + d, left, v[j]);
+            load_some<V>((const T *)a.x + (start + p) * a.ld_x + d, left, v[j]);
         else if (a.state_in && len >= 0)
-            load_some<8>((const T *)a.state_in + (slot * (W - 1) + len + j) * a.D + d, left, v[j]);
+            load_some<V>((const T *)a.state_in + (slot * (W - 1) + len + j) * a.D + d, left, v[j]);
         else
-            load_some<8>((const T *)a.x, 0, v[j]);
+            load_some<V>((const T *)a.x, 0, v[j]);
     }
 #pragma unroll
     for (int j = 0; j < W - 1; ++j)
-        store_some<8>((T *)a.state_out + (slot * (W - 1) + j) * a.D + d, left, v[j]);
+        store_some<V>((T *)a.state_out + (slot * (W - 1) + j) * a.D + d, left, v[j]);
 }
 
-// Workgroups first .. first + row_blocks - 1 convolve, those from row_blocks on
-// write states.
+template <int W, int V, bool FULL, typename T>
+__device__ __forceinline__ void conv_run(const ConvArgs &a, const Sequences &q, int64_t t0,
+                                         int64_t t1, int d, int left, bool together)
+{
+    const T *x = (const T *)a.x + d;
+    T *out = (T *)a.out + d;
+    const int64_t last = a.T - 1;
+    Raw<T, V> rows[kPiece], before[W - 1];
+    float k[W][V], bias[V];
+    // (a run's first rows are known before its sequence is)
+    load_rows_before<W, V, T>(a, t0, d, left, before);
+    const uint32_t bytes = (uint32_t)(a.ld_x * (int64_t)sizeof(T));
+    auto load = [&](int64_t t) {
+        const int there = (int)(last - t < kPiece ? last - t : kPiece);
+        const T *p = x + t * a.ld_x;
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i)
+            load_row<FULL, V>(row_at(p, i, there, bytes), left, rows[i]);
+    };
+    load(t0);
+    load_taps<W, V>(a.weight, d, left, k);
+    load_some<V>(a.bias ? a.bias + d : a.bias, a.bias ? left : 0, bias);
+    Segment seg;
+    seg.enter(q, t0, together);
+    for (int64_t t = t0;;) {
+        const int64_t end = seg.end < t1 ? seg.end : t1;
+        const int n = (int)(end - t);
+        float win[W - 1][V];
+        window_of<W, V, T>(a, seg, t, d, left, before, win);
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) {
+            float cur[V], y[V];
+            rows[i].unpack(cur);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float v = bias[e];
+#pragma unroll
+                for (int w = 0; w < W - 1; ++w)
+                    v += k[w][e] * win[w][e];
+                v += k[W - 1][e] * cur[e];
+                y[e] = a.silu ? silu(v) : v;
+#pragma unroll
+                for (int w = 0; w < W - 2; ++w)
+                    win[w][e] = win[w + 1][e];
+                win[W - 2][e] = cur[e];
+            }
+            if (i < n)
+                store_row<FULL, V>(out + (t + i) * a.ld_out, left, y);
+        }
+        t = end;
+        if (t >= t1)
+            break;
+        // another sequence begins within the run
+        seg.advance(q);
+        load_rows_before<W, V, T>(a, t, d, left, before);
+        load(t);
+    }
+}
+
+// Workgroups up to row_blocks convolve, those from row_blocks on write states.
 template <int W, typename T>
 __global__ __launch_bounds__(256) void conv_kernel(const ConvArgs a, const Cut c, int64_t first)
 {
-    constexpr int V = 8;
+    constexpr int V = 16 / sizeof(T);
     const Sequences q = {a.offsets, a.T, a.B, a.B > 0 ? a.T / a.B : 0};
-    const int d = ((int)blockIdx.y * c.lanes + threadIdx.x % c.lanes) * V, left = a.D - d;
+    int d = ((int)blockIdx.y * c.lanes + threadIdx.x % c.lanes) * V, left = a.D - d;
     if (left <= 0)
         return;
     const int64_t block = first + blockIdx.x;
@@ -114,62 +231,25 @@ __global__ __launch_bounds__(256) void conv_kernel(const ConvArgs a, const Cut c
     if (block >= c.row_blocks) {
         const int64_t s = run - c.row_blocks * c.runs;
         if (s < a.B)
-            write_state<W, T>(a, q, s, d, left);
+            write_state<W, V, T>(a, q, s, d, left);
         return;
     }
     const int64_t t0 = run * c.tokens, t1 = t0 + c.tokens < a.T ? t0 + c.tokens : a.T;
     if (t0 >= t1)
         return;
-    const T *x = (const T *)a.x + d;
-    T *out = (T *)a.out + d;
-    float k[W][V], bias[V], win[W - 1][V];
-    Raw<T, V> next[kBatch];
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b)
-        next[b].load(x + (t0 + b) * a.ld_x, t0 + b < t1 ? left : 0);
-    load_taps<W, V>(a.weight, d, left, k);
-    load_some<V>(a.bias ? a.bias + d : a.bias, a.bias ? left : 0, bias);
-    Segment seg;
-    seg.enter(q, t0);
-    load_window<W, V, T>(a, seg, t0, d, left, win);
-    for (int64_t t = t0; t < t1; t += kBatch) {
-        float cur[kBatch][V];
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            next[b].unpack(cur[b]);
-            next[b].load(x + (t + kBatch + b) * a.ld_x, t + kBatch + b < t1 ? left : 0);
-        }
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            if (t + b >= t1)
-                break;
-            if (t + b == seg.end) {
-                seg.advance(q);
-                load_window<W, V, T>(a, seg, t + b, d, left, win);
-            }
-            float y[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float v = bias[i];
-#pragma unroll
-                for (int w = 0; w < W - 1; ++w)
-                    v += k[w][i] * win[w][i];
-                v += k[W - 1][i] * cur[b][i];
-                y[i] = a.silu ? silu(v) : v;
-#pragma unroll
-                for (int w = 0; w < W - 2; ++w)
-                    win[w][i] = win[w + 1][i];
-                win[W - 2][i] = cur[b][i];
-            }
-            store_some<V>(out + (t + b) * a.ld_out, left, y);
-        }
-    }
+    whole_vector<V>(a.D, &d, &left);
+    // a wavefront along the channels has one run, unless the channels end in it
+    const bool together = c.lanes == 64 && __all(left >= V) && __popcll(__ballot(true)) == 64;
+    if (left >= V)
+        conv_run<W, V, true, T>(a, q, t0, t1, d, left, together);
+    else
+        conv_run<W, V, false, T>(a, q, t0, t1, d, left, together);
 }
 
 template <int W, typename T>
 __global__ __launch_bounds__(256) void conv_step_kernel(const ConvArgs a)
 {
-    constexpr int V = 8;
+    constexpr int V = 16 / sizeof(T);
     const int64_t vec = (a.D + V - 1) / V;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t row = id / vec;
@@ -199,16 +279,168 @@ __global__ __launch_bounds__(256) void conv_step_kernel(const ConvArgs a)
             store_some<V>((T *)a.state_out + (slot * (W - 1) + j) * a.D + d, left, v[j + 1]);
 }
 
-// Gradient.  Walking forward, token t adds dv_t weight_{W-1-j} to the gradient
-// of token t - j, j = 0 .. W - 1, so that of token t - (W - 1) is then whole.  A
-// run walks up to W - 1 tokens past its end to complete its own; the run that
-// holds a sequence's first token completes the gradient of its old state.
+// Gradient of a piece: with v the convolution and dv = dout f'(v), token t receives
+// dx_t = sum_j dv_{t+j} weight_{W-1-j} over the tokens t + j of its sequence, and its old
+// state the same of the tokens that read it.
+//
+// Rows t .. t + n - 1 of one sequence, all rows loaded at once; dv is formed for the W - 1
+// rows after them too.  Neither the old nor the new state takes part.
+template <int W, int V, typename T>
+__device__ __forceinline__ void backward_piece(const ConvArgs &a, const Segment &seg, int64_t t,
+                                               int n, int d, const float (&k)[W][V],
+                                               const float (&bias)[V], float (&sums)[W + 1][V])
+{
+    constexpr int PIECE = backward_piece_rows<T>(), ROWS = PIECE + W - 1;
+    const T *x = (const T *)a.x + d, *dy = (const T *)a.dout + d;
+    T *dx = (T *)a.out + d;
+    const int64_t last = a.T - 1;
+    Raw<T, V> rx[ROWS], ry[ROWS];
+    const int there = (int)(last - t < ROWS ? last - t : ROWS);
+    const uint32_t bx = (uint32_t)(a.ld_x * (int64_t)sizeof(T));
+    const uint32_t by = (uint32_t)(a.ld_dout * (int64_t)sizeof(T));
+    const T *px = x + t * a.ld_x, *py = dy + t * a.ld_dout;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        rx[i].load(row_at(px, i, there, bx), V);
+        ry[i].load(row_at(py, i, there, by), V);
+        if (i % 4 == 3)  // (the addresses of all rows at once would take the registers)
+            __builtin_amdgcn_sched_barrier(0);
+    }
+    Raw<T, V> before[W - 1];
+    load_rows_before<W, V, T>(a, t, d, V, before);
+    float win[W - 1][V], dv[W][V];  // dv: of the last W rows, the newest last
+    window_of<W, V, T>(a, seg, t, d, V, before, win);
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            dv[w][e] = 0.f;
+    const int reach = seg.end - t < ROWS ? (int)(seg.end - t) : ROWS;  // rows of the sequence
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        __builtin_amdgcn_sched_barrier(0);  // one row's values widened at a time
+        float cx[V], cy[V], whole[V];
+        rx[i].unpack(cx);
+        ry[i].unpack(cy);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            float v = bias[e];
+#pragma unroll
+            for (int w = 0; w < W - 1; ++w)
+                v += k[w][e] * win[w][e];
+            v += k[W - 1][e] * cx[e];
+            float g = cy[e];
+            if (a.silu)
+                g *= silu_slope(v, sigmoid(v));
+            g = i < reach ? g : 0.f;
+            if (i < PIECE) {
+                const float mine = i < n ? g : 0.f;
+#pragma unroll
+                for (int w = 0; w < W - 1; ++w)
+                    sums[w][e] += mine * win[w][e];
+                sums[W - 1][e] += mine * cx[e];
+                sums[W][e] += mine;
+            }
+#pragma unroll
+            for (int w = 0; w < W - 1; ++w)
+                dv[w][e] = dv[w + 1][e];
+            dv[W - 1][e] = g;
+#pragma unroll
+            for (int w = 0; w < W - 2; ++w)
+                win[w][e] = win[w + 1][e];
+            win[W - 2][e] = cx[e];
+            whole[e] = 0.f;  // row i - (W - 1), which is now whole
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                whole[e] += dv[j][e] * k[W - 1 - j][e];
+        }
+        const int r = i - (W - 1);
+        if (r >= 0 && r < n)
+            store_all<V>(dx + (t + r) * a.ld_out, whole);
+    }
+}
+
+// The same token by token, for any piece: the old state's gradient where the piece
+// begins with its sequence, the new state's where it holds tokens of it, and the
+// first `left` channels only.  (Rows a sequence's ends touch, and rows narrower
+// than a vector.)
+template <int W, int V, typename T>
+__device__ __forceinline__ void backward_edge(const ConvArgs &a, const Segment &seg, int64_t t, int n,
+                                           int d, int left, const float (&k)[W][V],
+                                           const float (&bias)[V], float (&sums)[W + 1][V])
+{
+    const T *x = (const T *)a.x + d, *dy = (const T *)a.dout + d;
+    T *dx = (T *)a.out + d;
+    const int64_t len = seg.end - seg.start, state = seg.seq * (W - 1);
+    Raw<T, V> before[W - 1];
+    load_rows_before<W, V, T>(a, t, d, left, before);
+    float win[W - 1][V], dv[W][V];
+    window_of<W, V, T>(a, seg, t, d, left, before, win);
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            dv[w][e] = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < n + W - 1; ++i) {
+        const bool there = t + i < seg.end;
+        float cx[V], cy[V], whole[V];
+        load_some<V>(x + (there ? (t + i) * a.ld_x : 0), there ? left : 0, cx);
+        load_some<V>(dy + (there ? (t + i) * a.ld_dout : 0), there ? left : 0, cy);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            float v = bias[e];
+#pragma unroll
+            for (int w = 0; w < W - 1; ++w)
+                v += k[w][e] * win[w][e];
+            v += k[W - 1][e] * cx[e];
+            float g = cy[e];
+            if (a.silu)
+                g *= silu_slope(v, sigmoid(v));
+            g = there ? g : 0.f;
+            const bool mine = there && i < n;
+#pragma unroll
+            for (int w = 0; w < W - 1; ++w)
+                sums[w][e] += mine ? g * win[w][e] : 0.f;
+            sums[W - 1][e] += mine ? g * cx[e] : 0.f;
+            sums[W][e] += mine ? g : 0.f;
+#pragma unroll
+            for (int w = 0; w < W - 1; ++w)
+                dv[w][e] = dv[w + 1][e];
+            dv[W - 1][e] = g;
+#pragma unroll
+            for (int w = 0; w < W - 2; ++w)
+                win[w][e] = win[w + 1][e];
+            win[W - 2][e] = cx[e];
+            whole[e] = 0.f;
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                whole[e] += dv[j][e] * k[W - 1 - j][e];
+        }
+        // Row i - (W - 1) of the piece is whole, as row `p` of the old state followed
+        // by the sequence, of which the last W - 1 rows are the new state.
+        const int r = i - (W - 1);
+        const int64_t p = (W - 1) + (t + r - seg.start);
+        if ((r < 0 && (t != seg.start || !a.state_out)) || r >= n)
+            continue;
+        if (a.dstate_out && p >= len) {
+            float o[V];
+            load_some<V>((const T *)a.dstate_out + (state + p - len) * a.D + d, left, o);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                whole[e] += o[e];
+        }
+        T *to = r < 0 ? (T *)a.state_out + (state + p) * a.D + d : dx + (t + r) * a.ld_out;
+        store_some<V>(to, left, whole);
+    }
+}
+
 template <int W, typename T>
 __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvArgs a, const Cut c)
 {
     constexpr int V = 4;
     const Sequences q = {a.offsets, a.T, a.B, a.B > 0 ? a.T / a.B : 0};
-    const int d = ((int)blockIdx.y * c.lanes + threadIdx.x % c.lanes) * V, left = a.D - d;
+    int d = ((int)blockIdx.y * c.lanes + threadIdx.x % c.lanes) * V, left = a.D - d;
     const int64_t run = (int64_t)blockIdx.x * c.runs + threadIdx.x / c.lanes;
     if ((int64_t)blockIdx.x >= c.row_blocks) {
         // the states of empty sequences pass through
@@ -224,6 +456,9 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvArgs a, co
         }
         return;
     }
+    const bool live = left > 0;
+    if (live)
+        whole_vector<V>(a.D, &d, &left);
     const int64_t t0 = run * c.tokens, t1 = t0 + c.tokens < a.T ? t0 + c.tokens : a.T;
     float sums[W + 1][V];  // dweight, dbias
 #pragma unroll
@@ -231,117 +466,24 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvArgs a, co
 #pragma unroll
         for (int i = 0; i < V; ++i)
             sums[w][i] = 0.f;
-    if (left > 0 && t0 < t1) {
-        const T *x = (const T *)a.x + d, *dy = (const T *)a.dout + d;
-        T *dx = (T *)a.out + d;
-        float k[W][V], bias[V], win[W - 1][V], wait[W - 1][V];
-        Raw<T, V> nx[kBatch], ny[kBatch];
-        const int64_t last = t1 + W - 1 < a.T ? t1 + W - 1 : a.T;  // rows that may be walked
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            const int n = t0 + b < last ? left : 0;
-            nx[b].load(x + (t0 + b) * a.ld_x, n);
-            ny[b].load(dy + (t0 + b) * a.ld_dout, n);
-        }
+    if (live && t0 < t1) {
+        float k[W][V], bias[V];
         load_taps<W, V>(a.weight, d, left, k);
         load_some<V>(a.bias ? a.bias + d : a.bias, a.bias ? left : 0, bias);
         Segment seg;
-        seg.enter(q, t0);
-        load_window<W, V, T>(a, seg, t0, d, left, win);
-#pragma unroll
-        for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                wait[j][i] = 0.f;
-        bool done = false;
-        for (int64_t tb = t0; !done; tb += kBatch) {
-            float cx[kBatch][V], cy[kBatch][V];
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b) {
-                nx[b].unpack(cx[b]);
-                ny[b].unpack(cy[b]);
-                const int64_t t = tb + kBatch + b;
-                const int n = t < last ? left : 0;
-                nx[b].load(x + t * a.ld_x, n);
-                ny[b].load(dy + t * a.ld_dout, n);
-            }
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b) {
-                const int64_t t = tb + b;
-                if (done)
-                    break;
-                if (t == seg.end) {  // t < t1 here: else the walk has ended
-                    seg.advance(q);
-                    load_window<W, V, T>(a, seg, t, d, left, win);
-#pragma unroll
-                    for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-                        for (int i = 0; i < V; ++i)
-                            wait[j][i] = 0.f;
-                }
-                const bool own = t < t1;
-                float whole[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float v = bias[i];
-#pragma unroll
-                    for (int w = 0; w < W - 1; ++w)
-                        v += k[w][i] * win[w][i];
-                    v += k[W - 1][i] * cx[b][i];
-                    float g = cy[b][i];
-                    if (a.silu)
-                        g *= silu_slope(v, sigmoid(v));
-                    const float mine = own ? g : 0.f;
-#pragma unroll
-                    for (int w = 0; w < W - 1; ++w)
-                        sums[w][i] += mine * win[w][i];
-                    sums[W - 1][i] += mine * cx[b][i];
-                    sums[W][i] += mine;
-                    whole[i] = wait[W - 2][i] + g * k[0][i];
-#pragma unroll
-                    for (int j = W - 2; j > 0; --j)
-                        wait[j][i] = wait[j - 1][i] + g * k[W - 1 - j][i];
-                    wait[0][i] = g * k[W - 1][i];
-#pragma unroll
-                    for (int w = 0; w < W - 2; ++w)
-                        win[w][i] = win[w + 1][i];
-                    win[W - 2][i] = cx[b][i];
-                }
-                const bool starts = seg.start >= t0 && seg.start < t1;  // the sequence starts here
-                const int64_t row = t - (W - 1);
-                if (row >= seg.start) {
-                    if (row >= t0)
-                        store_some<V>(dx + row * a.ld_out, left, whole);
-                } else if (starts && a.state_out) {
-                    const int64_t j = (W - 1) + (row - seg.start);
-                    store_some<V>((T *)a.state_out + (seg.seq * (W - 1) + j) * a.D + d, left, whole);
-                }
-                if (t + 1 == seg.end) {
-                    // wait[j] belongs to row t - j, that is to row W - 2 - j of state_out
-#pragma unroll
-                    for (int j = 0; j < W - 1; ++j) {
-                        float v[V];
-                        const int64_t from = (seg.seq * (W - 1) + (W - 2 - j)) * a.D + d;
-                        load_some<V>((const T *)a.dstate_out + (a.dstate_out ? from : 0),
-                                     a.dstate_out ? left : 0, v);
-#pragma unroll
-                        for (int i = 0; i < V; ++i)
-                            v[i] += wait[j][i];
-                        const int64_t r = t - j;
-                        if (r >= seg.start) {
-                            if (r >= t0 && r < t1)
-                                store_some<V>(dx + r * a.ld_out, left, v);
-                        } else if (starts && a.state_out) {
-                            const int64_t m = (W - 1) + (r - seg.start);
-                            store_some<V>((T *)a.state_out + (seg.seq * (W - 1) + m) * a.D + d,
-                                          left, v);
-                        }
-                    }
-                    done = t + 1 >= t1;
-                } else {
-                    done = t + 1 >= last;
-                }
-            }
+        seg.enter(q, t0, c.lanes == 64 && __popcll(__ballot(true)) == 64);
+        for (int64_t t = t0; t < t1;) {
+            int64_t end = seg.end < t1 ? seg.end : t1;
+            end = end < t + backward_piece_rows<T>() ? end : t + backward_piece_rows<T>();
+            const bool edge = left < V || (a.state_out && t == seg.start) ||
+                              (a.dstate_out && end > seg.end - (W - 1));
+            if (edge)
+                backward_edge<W, V, T>(a, seg, t, (int)(end - t), d, left, k, bias, sums);
+            else
+                backward_piece<W, V, T>(a, seg, t, (int)(end - t), d, k, bias, sums);
+            t = end;
+            if (t == seg.end && t < t1)
+                seg.advance(q);
         }
     }
     // the runs of the workgroup together: partial[row block][w][d]
@@ -358,9 +500,11 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvArgs a, co
         const int dd = (int)blockIdx.y * cols + ch;
         if (dd >= a.D)
             continue;
+        // (the last lane's vector may have been moved back)
+        const int lane = ch / V, back = dd - ch % V + V > a.D && a.D >= V ? dd - ch % V + V - a.D : 0;
         float v = 0.f;
         for (int r = 0; r < c.runs; ++r)
-            v += all[w * V + ch % V][r * c.lanes + ch / V];
+            v += all[w * V + ch % V + back][r * c.lanes + lane];
         a.partial[((int64_t)blockIdx.x * (W + 1) + w) * a.D + dd] = v;
     }
 }
@@ -388,7 +532,7 @@ template <typename F> hipError_t by_taps(int32_t W, F &&f)
 
 template <typename T> hipError_t forward(const ConvArgs &a, hipStream_t stream)
 {
-    const Cut c = forward_cut(a.T, a.D);
+    const Cut c = forward_cut(a.T, a.D, sizeof(T) == 2);
     const int64_t states = a.state_out ? (a.B + c.runs - 1) / c.runs : 0;
     // In place, a state may be written only when every run has read it.
     const bool in_place = a.state_out && a.state_out == a.state_in;
@@ -406,7 +550,7 @@ template <typename T> hipError_t forward(const ConvArgs &a, hipStream_t stream)
 }
 template <typename T> hipError_t step(const ConvArgs &a, hipStream_t stream)
 {
-    const int64_t threads = a.T * ((a.D + 7) / 8);
+    const int64_t threads = a.T * ((a.D + 16 / sizeof(T) - 1) / (16 / sizeof(T)));
     return by_taps(a.W, [&](auto w) {
         conv_step_kernel<decltype(w)::value, T>
             <<<dim3((unsigned)((threads + 255) / 256)), 256, 0, stream>>>(a);

@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256, NS <= 4 ? 4 : 2) void scan_kernel(const SsmArg
     float h[NS], total = 0.f;
     int64_t t = t0;
     if constexpr (ENDS) {
-        seg.enter(q, t1 - 1);
+        seg.enter(q, t1 - 1, true);
         const bool leaves = seg.end > t1;
         if (tid == 0 && tile.tile == 0 && tile.group == 0)
             a.flags[r] = !leaves || seg.start >= t0 ? kStarts : 0;
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256, NS <= 4 ? 4 : 2) void scan_kernel(const SsmArg
             }
         }
     } else {
-        seg.enter(q, t0);
+        seg.enter(q, t0, true);
         if (seg.start < t0)
             load_states<NS>(part_of(a.ends + (r - 1) * dN, dn), nn, h);
         else

@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256, NS <= 2 ? 4 : (NS == 4 ? 3 : (NS == 8 ? 2 : 1)
     if (t0 >= t1)
         return;
     Segment seg;
-    seg.enter(q, t0);
+    seg.enter(q, t0, true);
     const bool entered = JOINED && seg.start < t0;  // by a sequence under way
     const bool through = entered && seg.end > t1;   // which also leaves it
     bool first = entered;                           // still in that sequence
@@ -323,7 +323,7 @@ __global__ __launch_bounds__(256, waves_of<T>(NS)) void gradient_kernel(const Ss
     int64_t lo, t;
     int n;
     auto enter = [&](int64_t last) {
-        seg.enter(q, last);
+        seg.enter(q, last, true);
         lo = seg.start > t0 ? seg.start : t0;
         const int64_t hi = seg.end < t1 ? seg.end : t1;
         t = lo + (hi - 1 - lo) / STEP * STEP;
