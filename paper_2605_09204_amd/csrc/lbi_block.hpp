@@ -191,6 +191,26 @@ template <int N> __device__ __forceinline__ uint32_t lanes_max(uint32_t x)
     return x;
 }
 
+// The address of a uniform one plus this lane's 32-bit offset.  The offset is made
+// opaque at each use: the compiler would otherwise form the sum with the loop's
+// invariant part ahead of the loop, two registers for every tensor.
+template <typename T> __device__ __forceinline__ T *lane_address(T *uniform, uint32_t bytes)
+{
+    asm volatile("" : "+v"(bytes));
+    return (T *)((char *)uniform + bytes);
+}
+
+// A value that all lanes of the wavefront have, in scalar registers.
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) |
+           (int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
+}
+
+// A value that is formed here, not where it is used (the compiler would sink sums
+// that nothing reads until a walk's end past the walk, and keep their terms).
+__device__ __forceinline__ void pin(float &x) { asm volatile("" : "+v"(x)); }
+
 // 1 / (1 + e^-x); 0 and 1 at the ends of the range, NaN for NaN.
 __device__ __forceinline__ float sigmoid(float x)
 {

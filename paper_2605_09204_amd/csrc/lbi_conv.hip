@@ -13,8 +13,8 @@
 namespace lbi {
 namespace {
 
-constexpr int64_t kThreads = 1 << 17;  // threads wanted in all: eight wavefronts a CU
-constexpr int kPiece = 8;
+constexpr int64_t kThreads = 1 << 18;  // threads wanted in all: 16 wavefronts a CU
+constexpr int kPiece = 16;
 template <typename T> constexpr int backward_piece_rows() { return 32 / sizeof(T); }
 
 // How a [tokens][channels] plane is cut: lanes along the channels (a power of
@@ -23,27 +23,25 @@ struct Cut {
     int lanes, runs, tokens;
     int64_t row_blocks, col_blocks;
 };
-Cut cut_of(int64_t T, int32_t D, int V, int most_lanes, int least, int most)
+Cut cut_of(int64_t T, int32_t D, int V, int most)
 {
     const int64_t vec = (D + V - 1) / V;
     int lanes = 1;
-    while (lanes < most_lanes && lanes < vec)
+    while (lanes < 64 && lanes < vec)
         lanes *= 2;
-    int tokens = least;
+    int tokens = 4;
     while (tokens < most && T * vec > (int64_t)tokens * kThreads)
         tokens *= 2;
     const int runs = 256 / lanes;
     const int64_t per = (int64_t)runs * tokens;
     return {lanes, runs, tokens, (T + per - 1) / per, (vec + lanes - 1) / lanes};
 }
-// Forward: 16 bytes a lane.  Gradient: 4 channels a lane (its sums and its rows in
-// flight take twice the registers), and longer runs, which leave fewer partial sums.
-int forward_width(bool bf16) { return bf16 ? 8 : 4; }
-Cut forward_cut(int64_t T, int32_t D, bool bf16)
-{
-    return cut_of(T, D, forward_width(bf16), 64, 4, kPiece);
-}
-Cut backward_cut(int64_t T, int32_t D) { return cut_of(T, D, 4, 64, 4, 512); }
+// Two channels a lane: the rows in flight and, in the gradient, its sums then leave
+// room for four wavefronts a SIMD, which the operations need.  16384 tokens, 1536 channels,
+// bf16: forward 19 us (eight channels a lane 24), gradient 35 (four channels 46).
+constexpr int kWidth = 2;
+Cut forward_cut(int64_t T, int32_t D) { return cut_of(T, D, kWidth, kPiece); }
+Cut backward_cut(int64_t T, int32_t D) { return cut_of(T, D, kWidth, 512); }
 
 // The last vector of a row whose width is no multiple of V moves back to end with
 // the row: some channels are then computed twice, to the same values, and no lane
@@ -158,35 +156,51 @@ __device__ __forceinline__ void write_state(const ConvArgs &a, const Sequences &
         store_some<V>((T *)a.state_out + (slot * (W - 1) + j) * a.D + d, left, v[j]);
 }
 
-template <int W, int V, bool FULL, typename T>
+// A run, piece by piece.  UNIFORM: by a wavefront whose lanes all have the same run, so
+// that rows have uniform addresses.
+template <int W, int V, bool FULL, bool UNIFORM, typename T>
 __device__ __forceinline__ void conv_run(const ConvArgs &a, const Sequences &q, int64_t t0,
-                                         int64_t t1, int d, int left, bool together)
+                                         int64_t t1, int d, int left)
 {
-    const T *x = (const T *)a.x + d;
-    T *out = (T *)a.out + d;
     const int64_t last = a.T - 1;
+    const uint32_t lane = (uint32_t)d * sizeof(T), bytes = (uint32_t)(a.ld_x * (int64_t)sizeof(T));
     Raw<T, V> rows[kPiece], before[W - 1];
     float k[W][V], bias[V];
-    // (a run's first rows are known before its sequence is)
-    load_rows_before<W, V, T>(a, t0, d, left, before);
-    const uint32_t bytes = (uint32_t)(a.ld_x * (int64_t)sizeof(T));
+    if constexpr (UNIFORM) {
+        t0 = uniform(t0);
+        t1 = uniform(t1);
+    }
     auto load = [&](int64_t t) {
+        const T *p = (const T *)a.x + t * a.ld_x;
         const int there = (int)(last - t < kPiece ? last - t : kPiece);
-        const T *p = x + t * a.ld_x;
+        if constexpr (UNIFORM) {
 #pragma unroll
-        for (int i = 0; i < kPiece; ++i)
-            load_row<FULL, V>(row_at(p, i, there, bytes), left, rows[i]);
+            for (int j = 0; j < W - 1; ++j) {
+                const int64_t row = t - (W - 1) + j;
+                before[j].load(lane_address((const T *)a.x + (row > 0 ? row : 0) * a.ld_x, lane), V);
+            }
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i)
+                rows[i].load(lane_address(p + (i < there ? i : there) * a.ld_x, lane), V);
+        } else {
+            load_rows_before<W, V, T>(a, t, d, left, before);
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i)
+                load_row<FULL, V>(row_at(p + d, i, there, bytes), left, rows[i]);
+        }
     };
-    load(t0);
+    load(t0);  // the first rows are known before their sequence is
     load_taps<W, V>(a.weight, d, left, k);
     load_some<V>(a.bias ? a.bias + d : a.bias, a.bias ? left : 0, bias);
     Segment seg;
-    seg.enter(q, t0, together);
+    seg.enter(q, t0, UNIFORM);
     for (int64_t t = t0;;) {
-        const int64_t end = seg.end < t1 ? seg.end : t1;
+        int64_t end = seg.end < t1 ? seg.end : t1;
+        end = end < t + kPiece ? end : t + kPiece;
         const int n = (int)(end - t);
         float win[W - 1][V];
         window_of<W, V, T>(a, seg, t, d, left, before, win);
+        T *out = (T *)a.out + t * a.ld_out;
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) {
             float cur[V], y[V];
@@ -205,14 +219,13 @@ __device__ __forceinline__ void conv_run(const ConvArgs &a, const Sequences &q, 
                 win[W - 2][e] = cur[e];
             }
             if (i < n)
-                store_row<FULL, V>(out + (t + i) * a.ld_out, left, y);
+                store_row<FULL, V>(lane_address(out + i * a.ld_out, lane), left, y);
         }
         t = end;
         if (t >= t1)
             break;
-        // another sequence begins within the run
-        seg.advance(q);
-        load_rows_before<W, V, T>(a, t, d, left, before);
+        if (t == seg.end)
+            seg.advance(q);
         load(t);
     }
 }
@@ -221,12 +234,14 @@ __device__ __forceinline__ void conv_run(const ConvArgs &a, const Sequences &q, 
 template <int W, typename T>
 __global__ __launch_bounds__(256) void conv_kernel(const ConvArgs a, const Cut c, int64_t first)
 {
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = kWidth;
     const Sequences q = {a.offsets, a.T, a.B, a.B > 0 ? a.T / a.B : 0};
-    int d = ((int)blockIdx.y * c.lanes + threadIdx.x % c.lanes) * V, left = a.D - d;
+    const int64_t block_of = blockIdx.x / (unsigned)c.col_blocks;
+    const int col_block = (int)(blockIdx.x - block_of * c.col_blocks);
+    int d = (col_block * c.lanes + (int)threadIdx.x % c.lanes) * V, left = a.D - d;
     if (left <= 0)
         return;
-    const int64_t block = first + blockIdx.x;
+    const int64_t block = first + block_of;
     const int64_t run = block * c.runs + threadIdx.x / c.lanes;
     if (block >= c.row_blocks) {
         const int64_t s = run - c.row_blocks * c.runs;
@@ -239,11 +254,12 @@ __global__ __launch_bounds__(256) void conv_kernel(const ConvArgs a, const Cut c
         return;
     whole_vector<V>(a.D, &d, &left);
     // a wavefront along the channels has one run, unless the channels end in it
-    const bool together = c.lanes == 64 && __all(left >= V) && __popcll(__ballot(true)) == 64;
-    if (left >= V)
-        conv_run<W, V, true, T>(a, q, t0, t1, d, left, together);
+    if (left < V)
+        conv_run<W, V, false, false, T>(a, q, t0, t1, d, left);
+    else if (c.lanes == 64 && __popcll(__ballot(true)) == 64)
+        conv_run<W, V, true, true, T>(a, q, t0, t1, d, left);
     else
-        conv_run<W, V, false, T>(a, q, t0, t1, d, left, together);
+        conv_run<W, V, true, false, T>(a, q, t0, t1, d, left);
 }
 
 template <int W, typename T>
@@ -284,38 +300,58 @@ __global__ __launch_bounds__(256) void conv_step_kernel(const ConvArgs a)
 // state the same of the tokens that read it.
 //
 // Rows t .. t + n - 1 of one sequence, all rows loaded at once; dv is formed for the W - 1
-// rows after them too.  Neither the old nor the new state takes part.
-template <int W, int V, typename T>
+// rows after them too.  Neither the old nor the new state takes part.  WHOLE: a full
+// piece well within its sequence, the same for all lanes of the wavefront, so that rows
+// have uniform addresses and nothing is chosen by lane.
+template <int W, int V, bool WHOLE, typename T>
 __device__ __forceinline__ void backward_piece(const ConvArgs &a, const Segment &seg, int64_t t,
                                                int n, int d, const float (&k)[W][V],
                                                const float (&bias)[V], float (&sums)[W + 1][V])
 {
     constexpr int PIECE = backward_piece_rows<T>(), ROWS = PIECE + W - 1;
-    const T *x = (const T *)a.x + d, *dy = (const T *)a.dout + d;
-    T *dx = (T *)a.out + d;
-    const int64_t last = a.T - 1;
-    Raw<T, V> rx[ROWS], ry[ROWS];
-    const int there = (int)(last - t < ROWS ? last - t : ROWS);
-    const uint32_t bx = (uint32_t)(a.ld_x * (int64_t)sizeof(T));
-    const uint32_t by = (uint32_t)(a.ld_dout * (int64_t)sizeof(T));
-    const T *px = x + t * a.ld_x, *py = dy + t * a.ld_dout;
+    Raw<T, V> rx[ROWS], ry[ROWS], before[W - 1];
+    const uint32_t lane = (uint32_t)d * sizeof(T);
+    if constexpr (WHOLE) {
+        t = uniform(t);
+        const T *px = (const T *)a.x + t * a.ld_x, *py = (const T *)a.dout + t * a.ld_dout;
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        rx[i].load(row_at(px, i, there, bx), V);
-        ry[i].load(row_at(py, i, there, by), V);
-        if (i % 4 == 3)  // (the addresses of all rows at once would take the registers)
-            __builtin_amdgcn_sched_barrier(0);
+        for (int j = 0; j < W - 1; ++j)
+            before[j].load(lane_address(px - (W - 1 - j) * a.ld_x, lane), V);
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            rx[i].load(lane_address(px + i * a.ld_x, lane), V);
+            ry[i].load(lane_address(py + i * a.ld_dout, lane), V);
+        }
+    } else {
+        const int64_t last = a.T - 1;
+        const int there = (int)(last - t < ROWS ? last - t : ROWS);
+        const uint32_t bx = (uint32_t)(a.ld_x * (int64_t)sizeof(T));
+        const uint32_t by = (uint32_t)(a.ld_dout * (int64_t)sizeof(T));
+        const T *px = (const T *)a.x + t * a.ld_x + d, *py = (const T *)a.dout + t * a.ld_dout + d;
+        load_rows_before<W, V, T>(a, t, d, V, before);
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            rx[i].load(row_at(px, i, there, bx), V);
+            ry[i].load(row_at(py, i, there, by), V);
+            if (i % 4 == 3)  // (the addresses of all rows at once would take the registers)
+                __builtin_amdgcn_sched_barrier(0);
+        }
     }
-    Raw<T, V> before[W - 1];
-    load_rows_before<W, V, T>(a, t, d, V, before);
     float win[W - 1][V], dv[W][V];  // dv: of the last W rows, the newest last
-    window_of<W, V, T>(a, seg, t, d, V, before, win);
+    if constexpr (WHOLE) {
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j)
+            before[j].unpack(win[j]);
+    } else {
+        window_of<W, V, T>(a, seg, t, d, V, before, win);
+    }
 #pragma unroll
     for (int w = 0; w < W; ++w)
 #pragma unroll
         for (int e = 0; e < V; ++e)
             dv[w][e] = 0.f;
     const int reach = seg.end - t < ROWS ? (int)(seg.end - t) : ROWS;  // rows of the sequence
+    T *out = (T *)a.out + t * a.ld_out;
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         __builtin_amdgcn_sched_barrier(0);  // one row's values widened at a time
@@ -332,14 +368,18 @@ __device__ __forceinline__ void backward_piece(const ConvArgs &a, const Segment 
             float g = cy[e];
             if (a.silu)
                 g *= silu_slope(v, sigmoid(v));
-            g = i < reach ? g : 0.f;
+            if (!WHOLE)
+                g = i < reach ? g : 0.f;
             if (i < PIECE) {
-                const float mine = i < n ? g : 0.f;
+                const float mine = WHOLE || i < n ? g : 0.f;
 #pragma unroll
                 for (int w = 0; w < W - 1; ++w)
                     sums[w][e] += mine * win[w][e];
                 sums[W - 1][e] += mine * cx[e];
                 sums[W][e] += mine;
+#pragma unroll
+                for (int w = 0; w <= W; ++w)
+                    pin(sums[w][e]);
             }
 #pragma unroll
             for (int w = 0; w < W - 1; ++w)
@@ -349,14 +389,15 @@ __device__ __forceinline__ void backward_piece(const ConvArgs &a, const Segment 
             for (int w = 0; w < W - 2; ++w)
                 win[w][e] = win[w + 1][e];
             win[W - 2][e] = cx[e];
-            whole[e] = 0.f;  // row i - (W - 1), which is now whole
+            // row i - (W - 1), which is now whole
+            whole[e] = dv[0][e] * k[W - 1][e];
 #pragma unroll
-            for (int j = 0; j < W; ++j)
+            for (int j = 1; j < W; ++j)
                 whole[e] += dv[j][e] * k[W - 1 - j][e];
         }
         const int r = i - (W - 1);
-        if (r >= 0 && r < n)
-            store_all<V>(dx + (t + r) * a.ld_out, whole);
+        if (r >= 0 && (WHOLE || r < n))
+            store_all<V>(lane_address(out + r * a.ld_out, lane), whole);
     }
 }
 
@@ -438,11 +479,13 @@ __device__ __forceinline__ void backward_edge(const ConvArgs &a, const Segment &
 template <int W, typename T>
 __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvArgs a, const Cut c)
 {
-    constexpr int V = 4;
+    constexpr int V = kWidth;
     const Sequences q = {a.offsets, a.T, a.B, a.B > 0 ? a.T / a.B : 0};
-    int d = ((int)blockIdx.y * c.lanes + threadIdx.x % c.lanes) * V, left = a.D - d;
-    const int64_t run = (int64_t)blockIdx.x * c.runs + threadIdx.x / c.lanes;
-    if ((int64_t)blockIdx.x >= c.row_blocks) {
+    const int64_t block_of = blockIdx.x / (unsigned)c.col_blocks;
+    const int col_block = (int)(blockIdx.x - block_of * c.col_blocks);
+    int d = (col_block * c.lanes + (int)threadIdx.x % c.lanes) * V, left = a.D - d;
+    const int64_t run = block_of * c.runs + threadIdx.x / c.lanes;
+    if (block_of >= c.row_blocks) {
         // the states of empty sequences pass through
         const int64_t s = run - c.row_blocks * c.runs;
         if (left <= 0 || s >= a.B || q.at(s + 1) > q.at(s))
@@ -471,16 +514,23 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvArgs a, co
         load_taps<W, V>(a.weight, d, left, k);
         load_some<V>(a.bias ? a.bias + d : a.bias, a.bias ? left : 0, bias);
         Segment seg;
-        seg.enter(q, t0, c.lanes == 64 && __popcll(__ballot(true)) == 64);
+        // a wavefront along the channels has one run, unless the channels end in it
+        constexpr int PIECE = backward_piece_rows<T>();
+        const bool together = c.lanes == 64 && __popcll(__ballot(true)) == 64;
+        seg.enter(q, t0, together);
         for (int64_t t = t0; t < t1;) {
             int64_t end = seg.end < t1 ? seg.end : t1;
-            end = end < t + backward_piece_rows<T>() ? end : t + backward_piece_rows<T>();
+            end = end < t + PIECE ? end : t + PIECE;
             const bool edge = left < V || (a.state_out && t == seg.start) ||
                               (a.dstate_out && end > seg.end - (W - 1));
+            const bool whole = together && end - t == PIECE && t - seg.start >= W - 1 &&
+                               seg.end - t >= PIECE + W - 1;
             if (edge)
                 backward_edge<W, V, T>(a, seg, t, (int)(end - t), d, left, k, bias, sums);
+            else if (whole)
+                backward_piece<W, V, true, T>(a, seg, t, (int)(end - t), d, k, bias, sums);
             else
-                backward_piece<W, V, T>(a, seg, t, (int)(end - t), d, k, bias, sums);
+                backward_piece<W, V, false, T>(a, seg, t, (int)(end - t), d, k, bias, sums);
             t = end;
             if (t == seg.end && t < t1)
                 seg.advance(q);
@@ -497,7 +547,7 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvArgs a, co
     const int cols = c.lanes * V;  // channels of the workgroup
     for (int e = threadIdx.x; e < (W + 1) * cols; e += 256) {
         const int w = e / cols, ch = e - w * cols;
-        const int dd = (int)blockIdx.y * cols + ch;
+        const int dd = col_block * cols + ch;
         if (dd >= a.D)
             continue;
         // (the last lane's vector may have been moved back)
@@ -505,7 +555,7 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(const ConvArgs a, co
         float v = 0.f;
         for (int r = 0; r < c.runs; ++r)
             v += all[w * V + ch % V + back][r * c.lanes + lane];
-        a.partial[((int64_t)blockIdx.x * (W + 1) + w) * a.D + dd] = v;
+        a.partial[(block_of * (W + 1) + w) * a.D + dd] = v;
     }
 }
 
@@ -532,7 +582,7 @@ template <typename F> hipError_t by_taps(int32_t W, F &&f)
 
 template <typename T> hipError_t forward(const ConvArgs &a, hipStream_t stream)
 {
-    const Cut c = forward_cut(a.T, a.D, sizeof(T) == 2);
+    const Cut c = forward_cut(a.T, a.D);
     const int64_t states = a.state_out ? (a.B + c.runs - 1) / c.runs : 0;
     // In place, a state may be written only when every run has read it.
     const bool in_place = a.state_out && a.state_out == a.state_in;
@@ -540,10 +590,10 @@ template <typename T> hipError_t forward(const ConvArgs &a, hipStream_t stream)
         const int64_t n = c.row_blocks + (in_place ? 0 : states);
         if (n > 0)
             conv_kernel<decltype(w)::value, T>
-                <<<dim3((unsigned)n, (unsigned)c.col_blocks), 256, 0, stream>>>(a, c, 0);
+                <<<dim3((unsigned)(n * c.col_blocks)), 256, 0, stream>>>(a, c, 0);
         if (in_place && states > 0)
             conv_kernel<decltype(w)::value, T>
-                <<<dim3((unsigned)states, (unsigned)c.col_blocks), 256, 0, stream>>>(a, c,
+                <<<dim3((unsigned)(states * c.col_blocks)), 256, 0, stream>>>(a, c,
                                                                                      c.row_blocks);
         return hipGetLastError();
     });
@@ -565,7 +615,7 @@ template <typename T> hipError_t backward(const ConvArgs &a, hipStream_t stream)
     return by_taps(a.W, [&](auto w) {
         if (n > 0)
             conv_backward_kernel<decltype(w)::value, T>
-                <<<dim3((unsigned)n, (unsigned)c.col_blocks), 256, 0, stream>>>(a, c);
+                <<<dim3((unsigned)(n * c.col_blocks)), 256, 0, stream>>>(a, c);
         return hipGetLastError();
     });
 }

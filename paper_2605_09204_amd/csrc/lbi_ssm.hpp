@@ -38,19 +38,6 @@ template <int V> __device__ __forceinline__ void steps_of(bool use_softplus, flo
     }
 }
 
-// The address of a uniform one plus this lane's 32-bit offset.  The offset is made
-// opaque at each use: the compiler would otherwise form the sum with the loop's
-// invariant part ahead of the loop, two registers for every tensor.
-template <typename T> __device__ __forceinline__ T *lane_address(T *uniform, uint32_t bytes)
-{
-    asm volatile("" : "+v"(bytes));
-    return (T *)((char *)uniform + bytes);
-}
-
-// A value that is formed here, not where it is used (the compiler would sink sums
-// that nothing reads until a walk's end past the walk, and keep their terms).
-__device__ __forceinline__ void pin(float &x) { asm volatile("" : "+v"(x)); }
-
 // The kernel's own arguments, read again from where they were passed: within a loop
 // over tiles, so that some fifty pointers and strides are not held in scalar
 // registers (of which there are 102; the compiler spilled them to lanes of vector
