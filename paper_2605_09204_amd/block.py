@@ -93,112 +93,120 @@ def load() -> ctypes.CDLL:
     return lib
 
 
+# The checks below are what a small call spends most of its host time on: they compare with `is`
+# and by device index, and take shapes and strides once.
+
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _rows(name: str, t: torch.Tensor, lead, cols: int, dtype, device) -> int:
-    """Checks a token tensor of shape lead + (cols,) and returns its row stride."""
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != (*lead, cols):
-        raise ValueError(f"{name} must be a {dtype} {(*lead, cols)} tensor on {device}, got "
+def _rows(name: str, t: torch.Tensor, shape, dtype, dev: int) -> int:
+    """Checks a token tensor and returns its row stride."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{name} must be a {dtype} {tuple(shape)} tensor on cuda:{dev}, got "
                          f"{t.dtype} {tuple(t.shape)} on {t.device}")
-    return _row_stride(name, t)
+    return _row_stride(name, shape, t.stride())
 
 
-def _row_stride(name: str, t: torch.Tensor) -> int:
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+def _row_stride(name: str, shape, stride) -> int:
+    """The stride between the rows of all tokens."""
+    if stride[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}: the values of a row must lie side by side")
-    if t.dim() == 2:
-        return t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if t.shape[1] > 1:
-        ld = t.stride(1)
-        if t.shape[0] > 1 and t.stride(0) != t.shape[1] * ld:
+    if len(shape) == 2:
+        return stride[0] if shape[0] > 1 else shape[1]
+    if shape[1] > 1:
+        if shape[0] > 1 and stride[0] != shape[1] * stride[1]:
             raise ValueError(f"{name}: the rows of all sequences must lie at one stride")
-        return ld
-    return t.stride(0) if t.shape[0] > 1 else t.shape[2]
+        return stride[1]
+    return stride[0] if shape[0] > 1 else shape[2]
 
 
-def _vector(name: str, t: Optional[torch.Tensor], shape, device, dtype=torch.float32):
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype
-                          or t.device != device or not t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous {dtype} {tuple(shape)} tensor on {device}")
-    return t
+def _vector(name: str, t: Optional[torch.Tensor], shape, dev: int, dtype=torch.float32):
+    """Checks a dense tensor (None passes) and returns its pointer."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} {tuple(shape)} tensor on "
+                         f"cuda:{dev}")
+    return t.data_ptr()
 
 
 def _tokens(name: str, x: torch.Tensor):
-    """(leading shape, width, tokens) of a token tensor."""
-    if x.dim() not in (2, 3) or x.dtype not in _DTYPES or not x.is_cuda:
+    """(shape, tokens, dtype, device index, row stride) of the token tensor that leads a call."""
+    shape, dtype = x.shape, x.dtype
+    if len(shape) not in (2, 3) or dtype not in _DTYPES or not x.is_cuda:
         raise ValueError(f"{name} must be a [T, D] or [B, L, D] float32/bfloat16 GPU tensor")
-    lead = tuple(x.shape[:-1])
-    return lead, int(x.shape[-1]), lead[0] if len(lead) == 1 else lead[0] * lead[1]
+    T = shape[0] if len(shape) == 2 else shape[0] * shape[1]
+    return shape, T, dtype, x.get_device(), _row_stride(name, shape, x.stride())
 
 
-def _batch(lead, offsets, sequences, device) -> int:
+def _batch(shape, offsets, sequences, dev: int) -> int:
     """The number of packed sequences."""
     if offsets is not None:
-        if len(lead) != 1:
+        if len(shape) != 2:
             raise ValueError("offsets go with packed [T, D] tensors")
-        if (offsets.dim() != 1 or offsets.numel() < 1 or offsets.dtype != torch.int64
-                or offsets.device != device or not offsets.is_contiguous()):
-            raise ValueError(f"offsets must be a contiguous int64 [B + 1] tensor on {device}")
         n = offsets.numel() - 1
+        if n < 0:
+            raise ValueError("offsets must hold at least one value")
+        _vector("offsets", offsets, (n + 1,), dev, torch.int64)
     else:
-        n = lead[0] if len(lead) == 2 else (1 if sequences is None else int(sequences))
+        n = shape[0] if len(shape) == 3 else (1 if sequences is None else int(sequences))
     if sequences is not None and int(sequences) != n:
         raise ValueError(f"sequences is {sequences}, the tensors hold {n}")
     return n
 
 
-def _states(name, t, slots, n, tail, dtype, device):
-    """Checks a state tensor: [n or slots' rows, *tail]."""
-    if t is None:
-        return
-    if (t.dim() != 1 + len(tail) or tuple(t.shape[1:]) != tail or t.dtype != dtype
-            or t.device != device or not t.is_contiguous() or (slots is None and t.shape[0] != n)):
-        raise ValueError(f"{name} must be a contiguous {dtype} "
-                         f"{(n if slots is None else 'slots', *tail)} tensor on {device}")
-
-
-def _slots(slots, states, n, device):
-    """(pointer, rows of the state tensors)."""
+def _states(state_in, state_out, slots, n: int, tail, dtype, dev: int, names=("state_in",
+                                                                            "state_out")):
+    """Checks the states ([n or the slots' rows, *tail], None passes) and the slots; returns
+    (state_in pointer, state_out pointer, slots pointer, rows)."""
+    rows, ptrs = n, []
+    if slots is not None:
+        some = state_in if state_in is not None else state_out
+        rows = 0 if some is None else some.shape[0]
+    for name, t in zip(names, (state_in, state_out)):
+        ptrs.append(_vector(name, t, (rows, *tail), dev, dtype))
     if slots is None:
-        return None, 0
-    if (slots.dim() != 1 or slots.numel() != n or slots.dtype != torch.int32
-            or slots.device != device or not slots.is_contiguous()):
-        raise ValueError(f"slots must be a contiguous int32 [{n}] tensor on {device}")
-    rows = {t.shape[0] for t in states if t is not None}
-    if len(rows) > 1:
-        raise ValueError("state_in and state_out must have the same number of rows")
-    return slots.data_ptr(), rows.pop() if rows else 0
+        return ptrs[0], ptrs[1], None, 0
+    return ptrs[0], ptrs[1], _vector("slots", slots, (n,), dev, torch.int32), rows
 
 
-def _scratch(need: int, workspace, device):
+def _scratch(need: int, workspace, dev: int):
     """(the workspace, its pointer and bytes), allocated when needed and not given."""
-    if workspace is None and need > 0:
-        workspace = torch.empty((need,), dtype=torch.uint8, device=device)
     if workspace is None:
-        return None, None, 0
+        if need == 0:
+            return None, None, 0
+        workspace = torch.empty((need,), dtype=torch.uint8, device=f"cuda:{dev}")
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(stream, dev: int) -> int:
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(dev)
+    return _stream_ptr(stream, torch.device("cuda", dev))
 
 
 # ---- norm --------------------------------------------------------------------
 
 def _norm_inputs(x, weight, residual, residual_out):
-    lead, D, T = _tokens("x", x)
-    dev = x.device
-    _vector("weight", weight, (D,), dev)
-    ld_x = _row_stride("x", x)
+    shape, T, dtype, dev, ld_x = _tokens("x", x)
+    D = shape[-1]
+    w = _vector("weight", weight, (D,), dev)
     if residual is None:
         if residual_out is not None:
             raise ValueError("residual_out goes with a residual")
-        return lead, D, T, ld_x, 0, 0, _DTYPES[x.dtype], None
-    if residual.dtype not in _DTYPES:
-        raise TypeError(f"residual must be float32 or bfloat16, got {residual.dtype}")
-    ld_r = _rows("residual", residual, lead, D, residual.dtype, dev)
+        return shape, D, T, dtype, dev, ld_x, w, 0, 0, _DTYPES[dtype], None
+    rt = residual.dtype
+    if rt not in _DTYPES:
+        raise TypeError(f"residual must be float32 or bfloat16, got {rt}")
+    ld_r = _rows("residual", residual, shape, rt, dev)
     if residual_out is None:
-        residual_out = torch.empty((*lead, D), dtype=residual.dtype, device=dev)
-    ld_o = _rows("residual_out", residual_out, lead, D, residual.dtype, dev)
-    return lead, D, T, ld_x, ld_r, ld_o, _DTYPES[residual.dtype], residual_out
+        residual_out = x.new_empty(shape, dtype=rt)
+    ld_o = _rows("residual_out", residual_out, shape, rt, dev)
+    return shape, D, T, dtype, dev, ld_x, w, ld_r, ld_o, _DTYPES[rt], residual_out
 
 
 def lbi_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None,
@@ -206,14 +214,14 @@ def lbi_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
                  residual_out: Optional[torch.Tensor] = None, stream=None):
     """(out, residual_out): the root-mean-square norm of s = x + residual, and s (None without a
     residual).  residual_out may be residual itself."""
-    lead, D, T, ld_x, ld_r, ld_o, rdt, residual_out = _norm_inputs(x, weight, residual,
-                                                                   residual_out)
+    shape, D, T, dtype, dev, ld_x, w, ld_r, ld_o, rdt, residual_out = _norm_inputs(
+        x, weight, residual, residual_out)
     if out is None:
-        out = torch.empty((*lead, D), dtype=x.dtype, device=x.device)
+        out = x.new_empty(shape)
     _check(load().lbi_rms_norm(
-        x.data_ptr(), ld_x, _ptr(residual), ld_r, weight.data_ptr(), out.data_ptr(),
-        _rows("out", out, lead, D, x.dtype, x.device), _ptr(residual_out), ld_o, T, D, eps,
-        _DTYPES[x.dtype], rdt, _stream_ptr(stream, x.device)))
+        x.data_ptr(), ld_x, _ptr(residual), ld_r, w, out.data_ptr(),
+        _rows("out", out, shape, dtype, dev), _ptr(residual_out), ld_o, T, D, eps,
+        _DTYPES[dtype], rdt, _stream(stream, dev)))
     return out, residual_out
 
 
@@ -224,21 +232,20 @@ def lbi_rms_norm_q8(x: torch.Tensor, weight: torch.Tensor,
                     residual_out: Optional[torch.Tensor] = None, stream=None):
     """(q, scales, residual_out): the norm's output in 8 bits, q * scale, with one float32 scale
     for each ``group`` features of a token (0: for the token)."""
-    lead, D, T, ld_x, ld_r, ld_o, rdt, residual_out = _norm_inputs(x, weight, residual,
-                                                                   residual_out)
+    shape, D, T, dtype, dev, ld_x, w, ld_r, ld_o, rdt, residual_out = _norm_inputs(
+        x, weight, residual, residual_out)
     if format not in _Q8_TYPES:
         raise ValueError(f"format must be LBI_Q8_E4M3 or LBI_Q8_INT8, got {format}")
-    ngroups = -(-D // group) if group > 0 else 1
+    groups = (*shape[:-1], -(-D // group) if group > 0 else 1)
     if q is None:
-        q = torch.empty((*lead, D), dtype=_Q8_TYPES[format], device=x.device)
+        q = x.new_empty(shape, dtype=_Q8_TYPES[format])
     if scales is None:
-        scales = torch.empty((*lead, ngroups), dtype=torch.float32, device=x.device)
-    _vector("scales", scales, (*lead, ngroups), x.device)
+        scales = x.new_empty(groups, dtype=torch.float32)
     _check(load().lbi_rms_norm_q8(
-        x.data_ptr(), ld_x, _ptr(residual), ld_r, weight.data_ptr(), q.data_ptr(),
-        _rows("q", q, lead, D, _Q8_TYPES[format], x.device), scales.data_ptr(),
-        _ptr(residual_out), ld_o, T, D, eps, group, format, _DTYPES[x.dtype], rdt,
-        _stream_ptr(stream, x.device)))
+        x.data_ptr(), ld_x, _ptr(residual), ld_r, w, q.data_ptr(),
+        _rows("q", q, shape, _Q8_TYPES[format], dev), _vector("scales", scales, groups, dev),
+        _ptr(residual_out), ld_o, T, D, eps, group, format, _DTYPES[dtype], rdt,
+        _stream(stream, dev)))
     return q, scales, residual_out
 
 
@@ -253,37 +260,35 @@ def lbi_rms_norm_backward(dout: torch.Tensor, s: torch.Tensor, weight: torch.Ten
                           workspace: Optional[torch.Tensor] = None, stream=None):
     """(ds, dweight): the gradient of what was normalised (of x and of residual alike), with
     ``dresidual`` added, and of the weight.  ds may be dresidual itself."""
-    lead, D, T = _tokens("dout", dout)
-    dev = dout.device
-    if s.dtype not in _DTYPES:
-        raise TypeError(f"s must be float32 or bfloat16, got {s.dtype}")
-    ld_s = _rows("s", s, lead, D, s.dtype, dev)
-    ld_r = 0 if dresidual is None else _rows("dresidual", dresidual, lead, D, s.dtype, dev)
-    _vector("weight", weight, (D,), dev)
+    shape, T, dtype, dev, ld_dout = _tokens("dout", dout)
+    D, st = shape[-1], s.dtype
+    if st not in _DTYPES:
+        raise TypeError(f"s must be float32 or bfloat16, got {st}")
+    ld_s = _rows("s", s, shape, st, dev)
+    ld_r = 0 if dresidual is None else _rows("dresidual", dresidual, shape, st, dev)
+    w = _vector("weight", weight, (D,), dev)
     if ds is None:
-        ds = torch.empty((*lead, D), dtype=s.dtype, device=dev)
+        ds = s.new_empty(shape)
     if dweight is None:
-        dweight = torch.empty((D,), dtype=torch.float32, device=dev)
-    _vector("dweight", dweight, (D,), dev)
-    workspace, w, wb = _scratch(lbi_rms_norm_backward_workspace_bytes(T, D), workspace, dev)
+        dweight = weight.new_empty((D,))
+    workspace, ws, wb = _scratch(load().lbi_rms_norm_backward_workspace_bytes(T, D), workspace, dev)
     _check(load().lbi_rms_norm_backward(
-        dout.data_ptr(), _row_stride("dout", dout), s.data_ptr(), ld_s, weight.data_ptr(),
-        _ptr(dresidual), ld_r, ds.data_ptr(), _rows("ds", ds, lead, D, s.dtype, dev),
-        dweight.data_ptr(), T, D, eps, _DTYPES[dout.dtype], _DTYPES[s.dtype], w, wb,
-        _stream_ptr(stream, dev)))
+        dout.data_ptr(), ld_dout, s.data_ptr(), ld_s, w, _ptr(dresidual), ld_r, ds.data_ptr(),
+        _rows("ds", ds, shape, st, dev), _vector("dweight", dweight, (D,), dev), T, D, eps,
+        _DTYPES[dtype], _DTYPES[st], ws, wb, _stream(stream, dev)))
     return ds, dweight
 
 
 # ---- convolution -------------------------------------------------------------
 
 def _conv_inputs(x, weight, bias):
-    lead, D, T = _tokens("x", x)
+    shape, T, dtype, dev, ld_x = _tokens("x", x)
+    D = shape[-1]
     if weight.dim() != 2:
         raise ValueError("weight must be [D, W]")
-    W = int(weight.shape[1])
-    _vector("weight", weight, (D, W), x.device)
-    _vector("bias", bias, (D,), x.device)
-    return lead, D, T, W, _row_stride("x", x)
+    W = weight.shape[1]
+    return (shape, D, T, dtype, dev, ld_x, W, _vector("weight", weight, (D, W), dev),
+            _vector("bias", bias, (D,), dev))
 
 
 def lbi_ssm_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -294,18 +299,14 @@ def lbi_ssm_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
     """The causal convolution of every channel with its W = 2 .. 4 taps weight [D, W] along the
     tokens of each sequence.  state_in, state_out [B, W - 1, D]: the tokens before each sequence
     and the last ones after it."""
-    lead, D, T, W, ld_x = _conv_inputs(x, weight, bias)
-    dev = x.device
-    n = _batch(lead, offsets, sequences, dev)
-    for name, t in (("state_in", state_in), ("state_out", state_out)):
-        _states(name, t, slots, n, (W - 1, D), x.dtype, dev)
-    sp, ns = _slots(slots, (state_in, state_out), n, dev)
+    shape, D, T, dtype, dev, ld_x, W, w, b = _conv_inputs(x, weight, bias)
+    n = _batch(shape, offsets, sequences, dev)
+    si, so, sp, ns = _states(state_in, state_out, slots, n, (W - 1, D), dtype, dev)
     if out is None:
-        out = torch.empty((*lead, D), dtype=x.dtype, device=dev)
+        out = x.new_empty(shape)
     _check(load().lbi_ssm_conv(
-        x.data_ptr(), ld_x, weight.data_ptr(), _ptr(bias), out.data_ptr(),
-        _rows("out", out, lead, D, x.dtype, dev), _ptr(state_in), _ptr(state_out), sp, ns,
-        _ptr(offsets), T, n, D, W, int(silu), _DTYPES[x.dtype], _stream_ptr(stream, dev)))
+        x.data_ptr(), ld_x, w, b, out.data_ptr(), _rows("out", out, shape, dtype, dev), si, so, sp,
+        ns, _ptr(offsets), T, n, D, W, int(silu), _DTYPES[dtype], _stream(stream, dev)))
     return out
 
 
@@ -323,23 +324,22 @@ def lbi_ssm_conv_backward(x: torch.Tensor, weight: torch.Tensor, dout: torch.Ten
                           workspace: Optional[torch.Tensor] = None, stream=None):
     """(dx, dweight, dbias, dstate_in): dbias None without a bias, dstate_in None without
     state_in."""
-    lead, D, T, W, ld_x = _conv_inputs(x, weight, bias)
-    dev = x.device
-    n = _batch(lead, offsets, sequences, dev)
-    for name, t in (("state_in", state_in), ("dstate_out", dstate_out)):
-        _states(name, t, None, n, (W - 1, D), x.dtype, dev)
-    ld_dout = _rows("dout", dout, lead, D, x.dtype, dev)
+    shape, D, T, dtype, dev, ld_x, W, w, b = _conv_inputs(x, weight, bias)
+    n = _batch(shape, offsets, sequences, dev)
+    si, so, _, _ = _states(state_in, dstate_out, None, n, (W - 1, D), dtype, dev,
+                           ("state_in", "dstate_out"))
+    ld_dout = _rows("dout", dout, shape, dtype, dev)
     if dx is None:
-        dx = torch.empty((*lead, D), dtype=x.dtype, device=dev)
-    dweight = torch.empty((D, W), dtype=torch.float32, device=dev)
-    dbias = None if bias is None else torch.empty((D,), dtype=torch.float32, device=dev)
+        dx = x.new_empty(shape)
+    dweight = weight.new_empty((D, W))
+    dbias = None if bias is None else bias.new_empty((D,))
     dstate_in = None if state_in is None else torch.empty_like(state_in)
-    workspace, w, wb = _scratch(lbi_ssm_conv_backward_workspace_bytes(T, D, W), workspace, dev)
+    workspace, ws, wb = _scratch(load().lbi_ssm_conv_backward_workspace_bytes(T, D, W), workspace,
+                                 dev)
     _check(load().lbi_ssm_conv_backward(
-        x.data_ptr(), ld_x, weight.data_ptr(), _ptr(bias), dout.data_ptr(), ld_dout,
-        _ptr(state_in), _ptr(dstate_out), dx.data_ptr(), _rows("dx", dx, lead, D, x.dtype, dev),
-        dweight.data_ptr(), _ptr(dbias), _ptr(dstate_in), _ptr(offsets), T, n, D, W, int(silu),
-        _DTYPES[x.dtype], w, wb, _stream_ptr(stream, dev)))
+        x.data_ptr(), ld_x, w, b, dout.data_ptr(), ld_dout, si, so, dx.data_ptr(),
+        _rows("dx", dx, shape, dtype, dev), dweight.data_ptr(), _ptr(dbias), _ptr(dstate_in),
+        _ptr(offsets), T, n, D, W, int(silu), _DTYPES[dtype], ws, wb, _stream(stream, dev)))
     return dx, dweight, dbias, dstate_in
 
 
@@ -348,61 +348,51 @@ def lbi_ssm_conv_step(x: torch.Tensor, weight: torch.Tensor, state_in: torch.Ten
                       silu: bool = True, slots: Optional[torch.Tensor] = None,
                       out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """One token for each of n sequences, x [n, D]; state_out may be state_in."""
-    lead, D, n, W, ld_x = _conv_inputs(x, weight, bias)
-    if len(lead) != 1:
+    shape, D, n, dtype, dev, ld_x, W, w, b = _conv_inputs(x, weight, bias)
+    if len(shape) != 2:
         raise ValueError("x must be [n, D]")
-    dev = x.device
-    for name, t in (("state_in", state_in), ("state_out", state_out)):
-        _states(name, t, slots, n, (W - 1, D), x.dtype, dev)
-    sp, ns = _slots(slots, (state_in, state_out), n, dev)
+    si, so, sp, ns = _states(state_in, state_out, slots, n, (W - 1, D), dtype, dev)
     if out is None:
-        out = torch.empty((n, D), dtype=x.dtype, device=dev)
+        out = x.new_empty(shape)
     _check(load().lbi_ssm_conv_step(
-        x.data_ptr(), ld_x, weight.data_ptr(), _ptr(bias), out.data_ptr(),
-        _rows("out", out, lead, D, x.dtype, dev), state_in.data_ptr(), state_out.data_ptr(), sp,
-        ns, n, D, W, int(silu), _DTYPES[x.dtype], _stream_ptr(stream, dev)))
+        x.data_ptr(), ld_x, w, b, out.data_ptr(), _rows("out", out, shape, dtype, dev), si, so, sp,
+        ns, n, D, W, int(silu), _DTYPES[dtype], _stream(stream, dev)))
     return out
 
 
 # ---- scan --------------------------------------------------------------------
 
-def _groups(name, t, lead, N, dtype, device):
+def _groups(name, t, lead, N: int, dtype, dev: int):
     """(row stride, groups) of B or C: [..., N] or [..., G, N]."""
-    if (t.dtype != dtype or t.device != device or t.shape[:len(lead)] != lead
-            or t.dim() - len(lead) not in (1, 2) or t.shape[-1] != N):
+    shape, stride, k = t.shape, t.stride(), len(lead)
+    if (t.dtype is not dtype or t.get_device() != dev or shape[:k] != lead
+            or len(shape) - k not in (1, 2) or shape[-1] != N):
         raise ValueError(f"{name} must be a {dtype} {(*lead, 'G', N)} or {(*lead, N)} tensor on "
-                         f"{device}")
-    G = 1
-    if t.dim() > len(lead) + 1:
-        G = int(t.shape[-2])
-        if G > 1 and t.stride(-2) != N:
-            raise ValueError(f"{name}: a token's values must lie side by side")
-        t = t.as_strided((*lead, G * N), (*t.stride()[:len(lead)], 1)) if t.stride(-1) == 1 or \
-            N == 1 else t.flatten(-2)
-    return _row_stride(name, t), G
+                         f"cuda:{dev}")
+    G = shape[k] if len(shape) > k + 1 else 1
+    if (N > 1 and stride[-1] != 1) or (G > 1 and stride[-2] != N):
+        raise ValueError(f"{name}: a token's values must lie side by side")
+    return _row_stride(name, (*lead, G * N), (*stride[:k], 1)), G
 
 
 def _scan_inputs(u, delta, A, B, C, skip, z, delta_bias, softplus, offsets, sequences, state_in):
-    lead, D, T = _tokens("u", u)
-    dev = u.device
+    """(the struct, shape, dtype, device index); state_in: its pointer."""
+    shape, T, dtype, dev, ld_u = _tokens("u", u)
+    D, lead = shape[-1], shape[:-1]
     if A.dim() != 2:
         raise ValueError("A must be [D, N]")
-    N = int(A.shape[1])
-    _vector("A", A, (D, N), dev)
-    _vector("skip", skip, (D,), dev)
-    _vector("delta_bias", delta_bias, (D,), dev)
-    ld_B, G = _groups("B", B, lead, N, u.dtype, dev)
-    ld_C, G2 = _groups("C", C, lead, N, u.dtype, dev)
+    N = A.shape[1]
+    ld_B, G = _groups("B", B, lead, N, dtype, dev)
+    ld_C, G2 = _groups("C", C, lead, N, dtype, dev)
     if G != G2:
         raise ValueError("B and C must have the same groups")
-    n = _batch(lead, offsets, sequences, dev)
-    si = SsmInputs(u.data_ptr(), _row_stride("u", u), delta.data_ptr(),
-                   _rows("delta", delta, lead, D, u.dtype, dev), _ptr(z),
-                   0 if z is None else _rows("z", z, lead, D, u.dtype, dev), B.data_ptr(), ld_B,
-                   C.data_ptr(), ld_C, A.data_ptr(), _ptr(skip), _ptr(delta_bias),
-                   _ptr(state_in), _ptr(offsets), T, n, D, N, G, int(softplus),
-                   _DTYPES[u.dtype])
-    return si, lead, dev
+    n = _batch(shape, offsets, sequences, dev)
+    return SsmInputs(
+        u.data_ptr(), ld_u, delta.data_ptr(), _rows("delta", delta, shape, dtype, dev), _ptr(z),
+        0 if z is None else _rows("z", z, shape, dtype, dev), B.data_ptr(), ld_B, C.data_ptr(),
+        ld_C, _vector("A", A, (D, N), dev), _vector("skip", skip, (D,), dev),
+        _vector("delta_bias", delta_bias, (D,), dev), state_in, _ptr(offsets), T, n, D, N, G,
+        int(softplus), _DTYPES[dtype]), shape, dtype, dev
 
 
 def lbi_ssm_scan_workspace_bytes(T: int, sequences: int, D: int, N: int, G: int,
@@ -422,18 +412,19 @@ def lbi_ssm_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch
     """The selective scan of u under the steps softplus(delta + delta_bias), A [D, N] and the
     tokens' B, C [..., G, N] (or [..., N]), gated by silu(z).  state_in, state_out [B, D, N]
     float32: the states before and after each sequence; they may be the same tensor."""
-    si, lead, dev = _scan_inputs(u, delta, A, B, C, skip, z, delta_bias, softplus, offsets,
-                                 sequences, state_in)
-    for name, t in (("state_in", state_in), ("state_out", state_out)):
-        _states(name, t, slots, si.sequences, (si.D, si.N), torch.float32, dev)
-    sp, ns = _slots(slots, (state_in, state_out), si.sequences, dev)
+    si, shape, dtype, dev = _scan_inputs(u, delta, A, B, C, skip, z, delta_bias, softplus, offsets,
+                                         sequences, None)
+    si.state_in, so, sp, ns = _states(state_in, state_out, slots, si.sequences, (si.D, si.N),
+                                      torch.float32, dev)
     if out is None:
-        out = torch.empty((*lead, si.D), dtype=u.dtype, device=dev)
-    need = lbi_ssm_scan_workspace_bytes(si.T, si.sequences, si.D, si.N, si.G, offsets is not None)
+        out = u.new_empty(shape)
+    lib = load()
+    need = lib.lbi_ssm_scan_workspace_bytes(si.T, si.sequences, si.D, si.N, si.G,
+                                            int(offsets is not None))
     workspace, w, wb = _scratch(need, workspace, dev)
-    _check(load().lbi_ssm_scan(
-        ctypes.byref(si), out.data_ptr(), _rows("out", out, lead, si.D, u.dtype, dev),
-        _ptr(state_out), sp, ns, w, wb, _stream_ptr(stream, dev)))
+    _check(lib.lbi_ssm_scan(
+        ctypes.byref(si), out.data_ptr(), _rows("out", out, shape, dtype, dev), so, sp, ns, w, wb,
+        _stream(stream, dev)))
     return out
 
 
@@ -455,40 +446,40 @@ def lbi_ssm_scan_backward(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor,
                           workspace: Optional[torch.Tensor] = None, stream=None) -> dict:
     """The gradients by input: "u", "delta", "A", "B", "C", "skip", "z", "delta_bias" and
     "state_in", None where the input is.  ``outputs``: tensors to write some of them to."""
-    si, lead, dev = _scan_inputs(u, delta, A, B, C, skip, z, delta_bias, softplus, offsets,
-                                 sequences, state_in)
-    for name, t in (("state_in", state_in), ("dstate_out", dstate_out)):
-        _states(name, t, None, si.sequences, (si.D, si.N), torch.float32, dev)
-    ld_dout = _rows("dout", dout, lead, si.D, u.dtype, dev)
-    grads = {}
+    si, shape, dtype, dev = _scan_inputs(u, delta, A, B, C, skip, z, delta_bias, softplus, offsets,
+                                         sequences, None)
+    si.state_in, so, _, _ = _states(state_in, dstate_out, None, si.sequences, (si.D, si.N),
+                                    torch.float32, dev, ("state_in", "dstate_out"))
+    ld_dout = _rows("dout", dout, shape, dtype, dev)
+    g = {} if outputs is None else dict(outputs)
     for name, t in (("u", u), ("delta", delta), ("A", A), ("B", B), ("C", C), ("skip", skip),
                     ("z", z), ("delta_bias", delta_bias), ("state_in", state_in)):
-        g = None if outputs is None else outputs.get(name)
         if t is None:
-            if g is not None:
+            if g.get(name) is not None:
                 raise ValueError(f"outputs[{name!r}]: there is no such input")
-        elif g is None:
-            g = torch.empty(t.shape, dtype=t.dtype, device=dev)
-        elif name in ("A", "skip", "delta_bias", "state_in"):
-            _vector(f"outputs[{name!r}]", g, t.shape, dev)
-        grads[name] = g
-    ld = {k: 0 if grads[k] is None else _rows(f"outputs[{k!r}]", grads[k], lead, si.D, u.dtype,
-                                              dev) for k in ("u", "delta", "z")}
-    for k in ("B", "C"):
-        ld[k], G = _groups(f"outputs[{k!r}]", grads[k], lead, si.N, u.dtype, dev)
-        if G != si.G:
-            raise ValueError(f"outputs[{k!r}] must have {si.G} groups")
-    sg = SsmGradients(grads["u"].data_ptr(), ld["u"], grads["delta"].data_ptr(), ld["delta"],
-                      _ptr(grads["z"]), ld["z"], grads["B"].data_ptr(), ld["B"],
-                      grads["C"].data_ptr(), ld["C"], grads["A"].data_ptr(),
-                      _ptr(grads["skip"]), _ptr(grads["delta_bias"]), _ptr(grads["state_in"]))
-    need = lbi_ssm_scan_backward_workspace_bytes(si.T, si.sequences, si.D, si.N, si.G,
-                                                 offsets is not None)
+            g[name] = None
+        elif g.get(name) is None:
+            g[name] = t.new_empty(t.shape)
+    ld_B, G = _groups("outputs['B']", g["B"], shape[:-1], si.N, dtype, dev)
+    ld_C, G2 = _groups("outputs['C']", g["C"], shape[:-1], si.N, dtype, dev)
+    if G != si.G or G2 != si.G:
+        raise ValueError(f"outputs['B'] and outputs['C'] must have {si.G} groups")
+    sg = SsmGradients(
+        g["u"].data_ptr(), _rows("outputs['u']", g["u"], shape, dtype, dev),
+        g["delta"].data_ptr(), _rows("outputs['delta']", g["delta"], shape, dtype, dev),
+        _ptr(g["z"]), 0 if z is None else _rows("outputs['z']", g["z"], shape, dtype, dev),
+        g["B"].data_ptr(), ld_B, g["C"].data_ptr(), ld_C,
+        _vector("outputs['A']", g["A"], (si.D, si.N), dev),
+        _vector("outputs['skip']", g["skip"], (si.D,), dev),
+        _vector("outputs['delta_bias']", g["delta_bias"], (si.D,), dev),
+        _vector("outputs['state_in']", g["state_in"], (si.sequences, si.D, si.N), dev))
+    lib = load()
+    need = lib.lbi_ssm_scan_backward_workspace_bytes(si.T, si.sequences, si.D, si.N, si.G,
+                                                     int(offsets is not None))
     workspace, w, wb = _scratch(need, workspace, dev)
-    _check(load().lbi_ssm_scan_backward(
-        ctypes.byref(si), dout.data_ptr(), ld_dout, _ptr(dstate_out), ctypes.byref(sg), w, wb,
-        _stream_ptr(stream, dev)))
-    return grads
+    _check(lib.lbi_ssm_scan_backward(ctypes.byref(si), dout.data_ptr(), ld_dout, so,
+                                     ctypes.byref(sg), w, wb, _stream(stream, dev)))
+    return g
 
 
 def lbi_ssm_scan_step(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
@@ -498,16 +489,15 @@ def lbi_ssm_scan_step(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: 
                       slots: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                       stream=None) -> torch.Tensor:
     """One token for each of n sequences, u [n, D]; state_out may be state_in."""
-    si, lead, dev = _scan_inputs(u, delta, A, B, C, skip, z, delta_bias, softplus, None,
-                                 u.shape[0], state_in)
-    if len(lead) != 1:
+    if u.dim() != 2:
         raise ValueError("u must be [n, D]")
-    for name, t in (("state_in", state_in), ("state_out", state_out)):
-        _states(name, t, slots, si.sequences, (si.D, si.N), torch.float32, dev)
-    sp, ns = _slots(slots, (state_in, state_out), si.sequences, dev)
+    si, shape, dtype, dev = _scan_inputs(u, delta, A, B, C, skip, z, delta_bias, softplus, None,
+                                         u.shape[0], None)
+    si.state_in, so, sp, ns = _states(state_in, state_out, slots, si.sequences, (si.D, si.N),
+                                      torch.float32, dev)
     if out is None:
-        out = torch.empty((lead[0], si.D), dtype=u.dtype, device=dev)
+        out = u.new_empty(shape)
     _check(load().lbi_ssm_scan_step(
-        ctypes.byref(si), out.data_ptr(), _rows("out", out, lead, si.D, u.dtype, dev),
-        state_out.data_ptr(), sp, ns, _stream_ptr(stream, dev)))
+        ctypes.byref(si), out.data_ptr(), _rows("out", out, shape, dtype, dev), so, sp, ns,
+        _stream(stream, dev)))
     return out

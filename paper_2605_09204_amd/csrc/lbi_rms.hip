@@ -293,8 +293,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_backward_kernel
 // Rows below which a workgroup takes a row of more than 512 features: with a
 // wavefront each, fewer rows leave most of the 1024 SIMDs without work.
 constexpr int64_t kFewRows = 1024;
-constexpr int64_t kBlocks = 4096;          // forward: 16 workgroups a CU
-constexpr int64_t kBackwardBlocks = 512;   // also the rows of partial sums
+constexpr int64_t kBlocks = 2048;           // forward: 8 workgroups a CU
+constexpr int64_t kBackwardBlocks = 1024;  // also the rows of partial sums
 
 struct Shape {
     int lanes, nv, rows;  // lanes of a row, vectors a lane, rows a workgroup
