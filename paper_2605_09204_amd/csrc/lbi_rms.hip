@@ -57,14 +57,14 @@ template <int LANES> __device__ __forceinline__ uint32_t row_max(uint32_t v, flo
     return v;
 }
 
-template <int FMT> __device__ __forceinline__ uint32_t quantize4(const float *v, float inv)
+template <int FMT> __device__ __forceinline__ uint32_t quantize4(const float *v, float scale)
 {
     float x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         constexpr float top = FMT == kE4M3 ? 448.f : 127.f;
-        x[i] = v[i] * inv;
-        // the product may round past the largest value; NaN passes through
+        x[i] = v[i] / scale;
+        // the quotient may round past the largest value; NaN passes through
         x[i] = x[i] > top ? top : (x[i] < -top ? -top : x[i]);
     }
     if constexpr (FMT == kE4M3) {
@@ -79,20 +79,21 @@ template <int FMT> __device__ __forceinline__ uint32_t quantize4(const float *v,
     }
 }
 
-// The scale of a group from the bits of its largest |out|, and its reciprocal.
-// Unsigned comparison of the bits ranks infinity and NaN above every number.
-template <int FMT> __device__ __forceinline__ float scale_of(uint32_t top, float *inv)
+// The scale of a group from the bits of its largest |out|, and what its values are
+// divided by.  Unsigned comparison of the bits ranks infinity and NaN above every
+// number.
+template <int FMT> __device__ __forceinline__ float scale_of(uint32_t top, float *by)
 {
     const float scale = bitsf(top) / (FMT == kE4M3 ? 448.f : 127.f);
     if (top >= 0x7F800000u) {
-        *inv = bitsf(0x7FC00000u);
-        return *inv;
+        *by = bitsf(0x7FC00000u);
+        return *by;
     }
     if (scale < 1.17549435e-38f) {
-        *inv = 0.f;
+        *by = INFINITY;  // every value becomes 0
         return 1.f;
     }
-    *inv = 1.f / scale;
+    *by = scale;
     return scale;
 }
 
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_kernel(const No
                 for (int i = 0; i < 8; ++i)
                     top[j] = umax(top[j], fbits(s[j][i]) & 0x7FFFFFFFu);
             }
-            float inv[NV];
+            float by[NV];
             float *scales = a.scales + row * a.ngroups;
             if (a.group == 0) {
                 uint32_t m = top[0];
@@ -172,10 +173,10 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_kernel(const No
                 for (int j = 1; j < NV; ++j)
                     m = umax(m, top[j]);
                 m = row_max<LANES>(m, red_max, parity);
-                const float scale = scale_of<FMT>(m, &inv[0]);
+                const float scale = scale_of<FMT>(m, &by[0]);
 #pragma unroll
                 for (int j = 1; j < NV; ++j)
-                    inv[j] = inv[0];
+                    by[j] = by[0];
                 if (lane == 0)
                     scales[0] = scale;
             } else {
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_kernel(const No
                         m = umax(m, fbits(xchg<7>(bitsf(m))));
                     if (a.group >= 128)
                         m = umax(m, fbits(xchg<8>(bitsf(m))));
-                    const float scale = scale_of<FMT>(m, &inv[j]);
+                    const float scale = scale_of<FMT>(m, &by[j]);
                     if (left[j] > 0 && (col[j] & (a.group - 1)) == 0)
                         scales[col[j] / a.group] = scale;
                 }
@@ -194,8 +195,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_kernel(const No
             uint8_t *o = (uint8_t *)a.out + row * a.ld_out;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                const uint32_t q0 = quantize4<FMT>(s[j], inv[j]);
-                const uint32_t q1 = quantize4<FMT>(s[j] + 4, inv[j]);
+                const uint32_t q0 = quantize4<FMT>(s[j], by[j]);
+                const uint32_t q1 = quantize4<FMT>(s[j] + 4, by[j]);
                 if (left[j] >= 8) {
                     typedef u2 u2_byte __attribute__((aligned(1)));
                     *(u2_byte *)(o + col[j]) = u2{q0, q1};

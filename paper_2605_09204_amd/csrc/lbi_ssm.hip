@@ -185,6 +185,8 @@ __global__ __launch_bounds__(256, NS <= 4 ? 4 : 2) void scan_kernel(const SsmArg
 #pragma unroll
             for (int k = k0; k < k0 + 4 * UNROLL; k += 4) {
                 float y[4];
+                if (ENDS)  // (in pairs: a long sum keeps more of its digits)
+                    total += (dx[k][c].x + dx[k + 1][c].x) + (dx[k + 2][c].x + dx[k + 3][c].x);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const f2 p = dx[k + j][c];
@@ -195,12 +197,10 @@ __global__ __launch_bounds__(256, NS <= 4 ? 4 : 2) void scan_kernel(const SsmArg
                         if (!ENDS)
                             cc[i] = bc[k + j][g][NS + i];
                     }
-                    if (ENDS)
-                        total += p.x;
                     y[j] = 0.f;
 #pragma unroll
                     for (int i = 0; i < NS; ++i) {
-                        h[i] = fmaf(__builtin_amdgcn_exp2f(p.x * A2[i]), h[i], p.y * b[i]);
+                        h[i] = fmaf(decay(p.x, A2[i]), h[i], p.y * b[i]);
                         if (!ENDS)
                             y[j] = fmaf(cc[i], h[i], y[j]);
                     }
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(const SsmArgs a)
         float y = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            h[i] = fmaf(__builtin_amdgcn_exp2f(v * (A2[i] * kLog2e)), h[i], x * b[i]);
+            h[i] = fmaf(decay(v, A2[i] * kLog2e), h[i], x * b[i]);
             y = fmaf(c[i], h[i], y);
         }
         if (row >= 0)

@@ -179,6 +179,8 @@ __global__ __launch_bounds__(256, NS <= 2 ? 4 : (NS == 4 ? 3 : (NS == 8 ? 2 : 1)
                 if (JOINED && open && g == 0 && c < tile.left)
                     a.mark_sums[m * in.D + tile.d0 + c] = total;
             }
+            if (JOINED)  // (in pairs: a long sum keeps more of its digits)
+                total += (dx[k][c].x + dx[k + 1][c].x) + (dx[k + 2][c].x + dx[k + 3][c].x);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const f2 p = dx[k + j][c];
@@ -188,18 +190,15 @@ __global__ __launch_bounds__(256, NS <= 2 ? 4 : (NS == 4 ? 3 : (NS == 8 ? 2 : 1)
                     b[i] = bc[k + j][g][i];
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
-                    w[i] = __builtin_amdgcn_exp2f(p.x * A2[i]);
+                    w[i] = decay(p.x, A2[i]);
                     h[i] = fmaf(w[i], h[i], p.y * b[i]);
                 }
-                if (JOINED) {
-                    total += p.x;
-                    if (heads) {
-                        const float e = es[k + j][c];
+                if (JOINED && heads) {
+                    const float e = es[k + j][c];
 #pragma unroll
-                        for (int i = 0; i < NS; ++i) {
-                            way[i] *= w[i];
-                            head[i] = fmaf(way[i], e * bc[k + j][g][NS + i], head[i]);
-                        }
+                    for (int i = 0; i < NS; ++i) {
+                        way[i] *= w[i];
+                        head[i] = fmaf(way[i], e * bc[k + j][g][NS + i], head[i]);
                     }
                 }
             }
@@ -437,12 +436,14 @@ __global__ __launch_bounds__(256, waves_of<T>(NS)) void gradient_kernel(const Ss
             const f2 p = dx[k][c];
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
-                const float v = __builtin_amdgcn_exp2f(p.x * A2[i]);
+                const float v = decay(p.x, A2[i]);
                 if constexpr (KEEP)
                     w[k][i] = v;
                 hs[k + 1][i] = fmaf(v, hs[k][i], p.y * bc[k][g][i]);
             }
         }
+        float part[NS];  // the step's share of dA
+        zero_states(part);
 #pragma unroll
         for (int k = STEP - 4; k >= 0; k -= 4) {
             // indexes that the compiler cannot tell from other ones, so that dx and bc
@@ -469,7 +470,7 @@ __global__ __launch_bounds__(256, waves_of<T>(NS)) void gradient_kernel(const Ss
                         const float b = bcs[i], cc = bcs[NS + i];
                         float dec;
                         if constexpr (KEEP) dec = w[kk][i];
-                        else dec = __builtin_amdgcn_exp2f(x.x * A2[i]);
+                        else dec = decay(x.x, A2[i]);
                         gr[i] = fmaf(e, cc, gr[i]);
                         sy[j] = fmaf(cc, hs[kk + 1][i], sy[j]);
                         sb[j] = fmaf(gr[i], b, sb[j]);
@@ -478,8 +479,8 @@ __global__ __launch_bounds__(256, waves_of<T>(NS)) void gradient_kernel(const Ss
                         gr[i] *= dec;
                         const float qq = gr[i] * hs[kk][i];
                         sa[j] = fmaf(qq, A2[i], sa[j]);
-                        dA[i] = fmaf(qq, x.x, dA[i]);
-                        pin(dA[i]);
+                        part[i] = fmaf(qq, x.x, part[i]);
+                        pin(part[i]);
                     }
                     pin(sy[j]);
                 }
@@ -500,6 +501,9 @@ __global__ __launch_bounds__(256, waves_of<T>(NS)) void gradient_kernel(const Ss
             if (in.z)
                 oy[k + g][c] = sum_states(sy);
         }
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+            dA[i] += part[i];
         if (piece) {
             const PassedArgs p = passed();
             if (whole && p->out.dstate_in)
@@ -560,8 +564,8 @@ __global__ __launch_bounds__(256, waves_of<T>(NS)) void gradient_kernel(const Ss
         // No barrier: what the threads write before the next one are entries of
         // dx and es that only they themselves read here, and bc, that none does.
     }
-    float *part = a.part_par + r * (dN + 2 * in.D);
-    store_states<NS>(part_of(part, dn), nn, dA);
+    float *par_row = a.part_par + r * (dN + 2 * in.D);
+    store_states<NS>(part_of(par_row, dn), nn, dA);
     __syncthreads();
     if (tid < 2 * kChannels && tid % kChannels < tile.left) {
         const int which = tid / kChannels, at = tid % kChannels;
@@ -569,7 +573,7 @@ __global__ __launch_bounds__(256, waves_of<T>(NS)) void gradient_kernel(const Ss
 #pragma unroll
         for (int x = 0; x < 256 / LANES_V; ++x)
             v += sums[which][x][at];
-        part[dN + which * in.D + tile.d0 + at] = v;
+        par_row[dN + which * in.D + tile.d0 + at] = v;
     }
 }
 
