@@ -134,8 +134,10 @@ def _vector(name: str, t: Optional[torch.Tensor], shape, dev: int, dtype=torch.f
 def _tokens(name: str, x: torch.Tensor):
     """(shape, tokens, dtype, device index, row stride) of the token tensor that leads a call."""
     shape, dtype = x.shape, x.dtype
-    if len(shape) not in (2, 3) or dtype not in _DTYPES or not x.is_cuda:
-        raise ValueError(f"{name} must be a [T, D] or [B, L, D] float32/bfloat16 GPU tensor")
+    if dtype not in _DTYPES:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {dtype}")
+    if len(shape) not in (2, 3) or not x.is_cuda:
+        raise ValueError(f"{name} must be a [T, D] or [B, L, D] GPU tensor")
     T = shape[0] if len(shape) == 2 else shape[0] * shape[1]
     return shape, T, dtype, x.get_device(), _row_stride(name, shape, x.stride())
 
