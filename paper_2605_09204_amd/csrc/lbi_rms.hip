@@ -84,7 +84,7 @@ template <int FMT> __device__ __forceinline__ uint32_t quantize4(const float *v,
 // number.
 template <int FMT> __device__ __forceinline__ float scale_of(uint32_t top, float *by)
 {
-    const float scale = bitsf(top) / (FMT == kE4M3 ? 448.f : 127.f);
+    const float scale = bitsf(top) * (FMT == kE4M3 ? 1.f / 448.f : 1.f / 127.f);
     if (top >= 0x7F800000u) {
         *by = bitsf(0x7FC00000u);
         return *by;
@@ -105,6 +105,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_kernel(const No
     __shared__ float red_max[LANES > 64 ? 2 * LANES / 64 : 1];
     const int lane = threadIdx.x % LANES;
     const int64_t stride = (int64_t)gridDim.x * ROWS;
+    const float over_D = 1.f / (float)a.D;
     int col[NV], left[NV];
     float w[NV][8];
 #pragma unroll
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_kernel(const No
             for (int i = 0; i < 8; ++i)
                 sum[0] += s[j][i] * s[j][i];
         row_sum<LANES>(sum, red, parity);
-        const float r = 1.f / sqrtf(sum[0] / (float)a.D + a.eps);
+        const float r = rsqrtf(sum[0] * over_D + a.eps);
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -219,6 +220,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_backward_kernel
     __shared__ float red[LANES > 64 ? 4 * LANES / 64 : 1];
     const int lane = threadIdx.x % LANES;
     const int64_t stride = (int64_t)gridDim.x * ROWS;
+    const float over_D = 1.f / (float)a.D;
     int col[NV], left[NV];
     float w[NV][8], dw[NV][8];
 #pragma unroll
@@ -251,8 +253,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_backward_kernel
                 sum[1] += s[j][i] * (g[j][i] * w[j][i]);
             }
         row_sum<LANES>(sum, red, parity);
-        const float r = 1.f / sqrtf(sum[0] / (float)a.D + a.eps);
-        const float m = sum[1] * r / (float)a.D;  // mean(g n)
+        const float r = rsqrtf(sum[0] * over_D + a.eps);
+        const float m = sum[1] * r * over_D;  // mean(g n)
         R *o = (R *)a.out + row * a.ld_out;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -291,22 +293,21 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_backward_kernel
     }
 }
 
-// Rows below which a workgroup takes a row of more than 512 features: with a
-// wavefront each, fewer rows leave most of the 1024 SIMDs without work.
-constexpr int64_t kFewRows = 1024;
-constexpr int64_t kBlocks = 2048;           // forward: 8 workgroups a CU
+constexpr int64_t kBlocks = 2048;          // forward: 8 workgroups a CU
 constexpr int64_t kBackwardBlocks = 1024;  // also the rows of partial sums
 
 struct Shape {
     int lanes, nv, rows;  // lanes of a row, vectors a lane, rows a workgroup
 };
-Shape shape_of(int64_t T, int32_t D)
+// Up to 1024 features a wavefront takes a row, above that a workgroup: measured in bf16
+// at 64 to 16384 rows, a workgroup instead costs rows of 1024 features 3 to 26 per cent forward
+// and up to 61 in the gradient, and a wavefront instead costs rows of 2048 up to 24 forward.
+Shape shape_of(int32_t D)
 {
     const int vec = (D + 7) / 8;
     if (vec <= 16) return {16, 1, 16};
     if (vec <= 64) return {64, 1, 4};
-    if (T >= kFewRows && vec <= 128) return {64, 2, 4};
-    if (T >= kFewRows && vec <= 256) return {64, 4, 4};
+    if (vec <= 128) return {64, 2, 4};
     if (vec <= 256) return {256, 1, 1};
     if (vec <= 512) return {256, 2, 1};
     if (vec <= 1024) return {256, 4, 1};
@@ -319,8 +320,7 @@ template <typename F> hipError_t by_shape(const Shape &s, F &&f)
     if (s.lanes == 16) return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
     if (s.lanes == 64) {
         if (s.nv == 1) return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
-        if (s.nv == 2) return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
-        return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
+        return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
     }
     if (s.lanes == 256) {
         if (s.nv == 1) return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
@@ -343,7 +343,7 @@ struct ToVector {
 template <typename X, typename R, int FMT>
 hipError_t forward(const NormArgs &a, hipStream_t stream)
 {
-    const Shape s = shape_of(a.T, a.D);
+    const Shape s = shape_of(a.D);
     const dim3 grid((unsigned)block_count(a.T, s.rows, kBlocks)), block(s.lanes < 256 ? 256 : s.lanes);
     return by_shape(s, [&](auto lanes, auto nv) {
         rms_kernel<X, R, decltype(lanes)::value, decltype(nv)::value, FMT>
@@ -362,7 +362,7 @@ hipError_t forward_types(const NormArgs &a, bool bf16, bool residual_bf16, hipSt
 }
 template <typename X, typename R> hipError_t backward(const NormArgs &a, hipStream_t stream)
 {
-    const Shape s = shape_of(a.T, a.D);
+    const Shape s = shape_of(a.D);
     const dim3 grid((unsigned)norm_partial_rows(a.T, a.D)), block(s.lanes < 256 ? 256 : s.lanes);
     return by_shape(s, [&](auto lanes, auto nv) {
         rms_backward_kernel<X, R, decltype(lanes)::value, decltype(nv)::value>
@@ -387,7 +387,11 @@ hipError_t launch_rms_norm_q8(const NormArgs &a, bool int8, bool bf16, bool resi
 
 int64_t norm_partial_rows(int64_t T, int32_t D)
 {
-    return block_count(T, shape_of(T, D).rows, kBackwardBlocks);
+    const int rows = shape_of(D).rows;
+    const int64_t n = block_count(T, rows, kBackwardBlocks);
+    // four rows a workgroup at least where that leaves one a CU: each writes a row of sums
+    const int64_t most = (T + 3) / 4 > 256 ? (T + 3) / 4 : 256;
+    return n < most ? n : most;
 }
 
 hipError_t launch_rms_norm_backward(const NormArgs &a, float *dweight, bool bf16,
