@@ -8,6 +8,10 @@
 // around a piece come from cache), a few operations for each: the bound is HBM.
 // Lanes of a workgroup lie along the channels (a row's values are contiguous) and,
 // above that, along the runs.
+//
+// Measured, four taps, bf16, 1536 channels: 8201 packed tokens of 13 sequences, 51 MB, in
+// 14.5 us (3.5 TB/s; a copy of as many bytes 8.4 us); the gradient of 16384 tokens, 151 MB,
+// in 34 + 4 us (4.0 TB/s); one token of 64 sequences 5.6 us, of which a launch is most.
 #include "lbi_block.hpp"
 
 namespace lbi {

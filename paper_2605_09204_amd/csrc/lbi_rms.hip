@@ -6,9 +6,16 @@
 // magnitudes; for the gradient, its dot product with g) is formed over the
 // lanes of the row, then the row is written.  So each form moves exactly the
 // bytes it has to, and the bound is HBM.  A group of LANES lanes owns a row: 16
-// for rows of up to 128 features, a wavefront up to 2048 where there are rows
-// enough to fill the GPU, and otherwise a workgroup, so that few rows still
-// have many loads in flight.
+// for rows of up to 128 features, a wavefront up to 1024, above that a workgroup.
+// The gradient of the weight is a sum over all rows: each workgroup adds its own in
+// registers, writes one row of sums, and a second kernel adds those in a fixed order.
+//
+// Everything is float32 until the one rounding to the output's type; an 8-bit value
+// is the float32 output over its scale, rounded to nearest even.
+//
+// Measured, bf16 with the residual: 16384 rows of 768 features, 101 MB: forward
+// 16 us (6.3 TB/s; a copy of as many bytes 15.7 us), gradient 20 + 4 us (4.1 TB/s);
+// 4099 rows of 2048 to E4M3 by groups of 128, 59 MB: 13.9 us (4.2 TB/s).
 #include "lbi_block.hpp"
 
 namespace lbi {
