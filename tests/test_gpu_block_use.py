@@ -137,6 +137,33 @@ def test_gradients_against_differences(kind):
     assert abs(got - want) <= DIFF_TOL * size
 
 
+# ---- many ranges ------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("lengths", [[700, 1, 0, 1400, 33, 64, 2], [4100, 31, 2500, 0, 900, 1700],
+                                     [9001], [3000, 3000]], ids=str)
+def test_scan_over_many_ranges(lengths):
+    """Few channels and many tokens are cut into tens to hundreds of ranges, with sequences that begin
+    anywhere in them; tolerances as for the short ones."""
+    from test_gpu_block import call_scan, check, packing, scan_inputs
+
+    D, N, G = 6, 5, 2
+    s, g = scan_inputs(lengths, D, N, G, "f32", sum(lengths))
+    T, S = sum(lengths), len(lengths)
+    assert block.lbi_ssm_scan_workspace_bytes(T, S, D, N, G, "offsets" in packing(lengths)) > 0
+    new = torch.full((S, D, N), float("nan"), device=DEV)
+    say(f"[many ranges] {lengths}")
+    y = call_scan(s, lengths, state_out=new)
+    want, want_new = ref.scan(s, lengths)
+    check(y, want, "y")
+    check(new, want_new, "state_out")
+    dout, dnew = torch.randn(T, D, generator=g).to(DEV), torch.randn(S, D, N, generator=g).to(DEV)
+    got = block.lbi_ssm_scan_backward(dout=dout, dstate_out=dnew, **s, **packing(lengths))
+    want = ref.scan_backward(s, lengths, dout, dnew)
+    for k, e in want.items():
+        check(got[k], e, k, want["delta"].norm().item() if k == "delta_bias" else None)
+
+
 # ---- addresses past 32 bits ------------------------------------------------------
 
 FAR = 1 << 23  # elements from row to row: 600 rows span 2^32 elements and more
