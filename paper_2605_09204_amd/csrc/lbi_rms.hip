@@ -15,7 +15,7 @@
 //
 // Measured, bf16 with the residual: 16384 rows of 768 features, 101 MB: forward
 // 16 us (6.3 TB/s; a copy of as many bytes 15.7 us), gradient 20 + 4 us (4.1 TB/s);
-// 4099 rows of 2048 to E4M3 by groups of 128, 59 MB: 13.9 us (4.2 TB/s).
+// 4099 rows of 2048 to E4M3 by groups of 128, 59 MB: 14 us (4.2 TB/s).
 #include "lbi_block.hpp"
 
 namespace lbi {
