@@ -90,12 +90,24 @@ lbi_status lbi_rms_norm(const void *x, int64_t ld_x, const void *residual, int64
  *   q       OUTPUT [T][D] bytes, at row stride ld_q: out / scale rounded to
  *           the nearest value of `format` (ties to even).
  *   scales  OUTPUT [T][ceil(D / group)] float32, dense: the largest |out| of
- *           the group's features / 448 (E4M3) or / 127 (INT8).  1 where that
- *           is below the smallest normal float32 (q is then 0), NaN where an
- *           out of the group is NaN or infinite.
+ *           the group's features times the float32 value of 1 / 448 (E4M3) or
+ *           1 / 127 (INT8).  1 where that is below the smallest normal float32
+ *           (q is then 0), NaN where an out of the group is NaN or infinite.
  *   group   features that share a scale: 32, 64 or 128, or 0 for the whole row
  *           (else LBI_ERR_SHAPE).
  *   format  an lbi_q8_format (else LBI_ERR_DTYPE).
+ *
+ * A quotient in the middle between two values of the format goes by the last
+ * bits of what it was computed from.  So each operation here is rounded to
+ * float32 by itself, (s * rsqrt(sum * (1 / D) + eps)) * weight, and the sum of
+ * the squares has a stated order.  D < 128: sum l of L = min(64, the largest
+ * power of two up to D) is that of elements l and l + L.  D >= 128: the row's
+ * aligned vectors of four, which begin where t D + d is a multiple of four, go
+ * to 64 lanes in turn; a lane's four sums (one an element of its vectors) grow
+ * along the row and are added in order; what lies ahead of the first vector or
+ * after the last joins the first sum of lanes (t D mod 4) .. 3 and 0 .. 2.  The
+ * L or 64 sums are added pairwise, neighbours first.  (For D no multiple of
+ * four a row's last bits thus go by its place t.)
  */
 lbi_status lbi_rms_norm_q8(const void *x, int64_t ld_x, const void *residual,
                            int64_t ld_residual, const float *weight, void *q, int64_t ld_q,
