@@ -6,6 +6,10 @@ Every function has the name of the C entry point it calls.  Token tensors are [T
 projection's output are taken as they are), the values of a row side by side.  Without
 ``offsets`` a [T, D] tensor holds ``sequences`` sequences of the same length.  Outputs and the
 workspace are allocated unless they are given.
+
+``stream`` (a torch stream or a handle): where the call runs instead of the current stream.  What the
+call allocates is that stream's own.  Waiting is left to the caller, in both directions, and so is
+keeping the inputs and the given tensors alive until the call is done.
 """
 from __future__ import annotations
 
@@ -185,10 +189,30 @@ def _scratch(need: int, workspace, dev: int):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream, dev: int) -> int:
-    if stream is None and _raw_stream is not None:
-        return _raw_stream(dev)
-    return _stream_ptr(stream, torch.device("cuda", dev))
+def _stream(dev: int) -> int:
+    """The current stream of the device, as the library takes it."""
+    return _raw_stream(dev) if _raw_stream is not None else _stream_ptr(None, torch.device("cuda", dev))
+
+
+def _aside(call, stream, x, *args, **outputs):
+    """The call on ``stream``, made the current one: what the call allocates then comes from that
+    stream's memory, in its order.  Results are recorded on the caller's stream, where they may be
+    used (behind a wait) and dropped."""
+    if not x.is_cuda:
+        return call(x, *args, **outputs)  # which refuses it
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=x.device) if int(stream) \
+            else torch.cuda.default_stream(x.device)
+    if stream.device != x.device:
+        raise ValueError(f"stream belongs to {stream.device}, the tensors to {x.device}")
+    here = torch.cuda.current_stream(x.device)
+    with torch.cuda.stream(stream):
+        results = call(x, *args, **outputs)
+    for t in (results.values() if isinstance(results, dict) else
+              results if isinstance(results, tuple) else (results,)):
+        if t is not None:
+            t.record_stream(here)
+    return results
 
 
 # ---- norm --------------------------------------------------------------------
@@ -216,6 +240,9 @@ def lbi_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
                  residual_out: Optional[torch.Tensor] = None, stream=None):
     """(out, residual_out): the root-mean-square norm of s = x + residual, and s (None without a
     residual).  residual_out may be residual itself."""
+    if stream is not None:
+        return _aside(lbi_rms_norm, stream, x, weight, residual, eps, out=out,
+                      residual_out=residual_out)
     shape, D, T, dtype, dev, ld_x, w, ld_r, ld_o, rdt, residual_out = _norm_inputs(
         x, weight, residual, residual_out)
     if out is None:
@@ -223,7 +250,7 @@ def lbi_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
     _check(load().lbi_rms_norm(
         x.data_ptr(), ld_x, _ptr(residual), ld_r, w, out.data_ptr(),
         _rows("out", out, shape, dtype, dev), _ptr(residual_out), ld_o, T, D, eps,
-        _DTYPES[dtype], rdt, _stream(stream, dev)))
+        _DTYPES[dtype], rdt, _stream(dev)))
     return out, residual_out
 
 
@@ -234,6 +261,9 @@ def lbi_rms_norm_q8(x: torch.Tensor, weight: torch.Tensor,
                     residual_out: Optional[torch.Tensor] = None, stream=None):
     """(q, scales, residual_out): the norm's output in 8 bits, q * scale, with one float32 scale
     for each ``group`` features of a token (0: for the token)."""
+    if stream is not None:
+        return _aside(lbi_rms_norm_q8, stream, x, weight, residual, eps, format, group, q=q,
+                      scales=scales, residual_out=residual_out)
     shape, D, T, dtype, dev, ld_x, w, ld_r, ld_o, rdt, residual_out = _norm_inputs(
         x, weight, residual, residual_out)
     if format not in _Q8_TYPES:
@@ -247,7 +277,7 @@ def lbi_rms_norm_q8(x: torch.Tensor, weight: torch.Tensor,
         x.data_ptr(), ld_x, _ptr(residual), ld_r, w, q.data_ptr(),
         _rows("q", q, shape, _Q8_TYPES[format], dev), _vector("scales", scales, groups, dev),
         _ptr(residual_out), ld_o, T, D, eps, group, format, _DTYPES[dtype], rdt,
-        _stream(stream, dev)))
+        _stream(dev)))
     return q, scales, residual_out
 
 
@@ -262,6 +292,9 @@ def lbi_rms_norm_backward(dout: torch.Tensor, s: torch.Tensor, weight: torch.Ten
                           workspace: Optional[torch.Tensor] = None, stream=None):
     """(ds, dweight): the gradient of what was normalised (of x and of residual alike), with
     ``dresidual`` added, and of the weight.  ds may be dresidual itself."""
+    if stream is not None:
+        return _aside(lbi_rms_norm_backward, stream, dout, s, weight, dresidual, eps, ds=ds,
+                      dweight=dweight, workspace=workspace)
     shape, T, dtype, dev, ld_dout = _tokens("dout", dout)
     D, st = shape[-1], s.dtype
     if st not in _DTYPES:
@@ -277,7 +310,7 @@ def lbi_rms_norm_backward(dout: torch.Tensor, s: torch.Tensor, weight: torch.Ten
     _check(load().lbi_rms_norm_backward(
         dout.data_ptr(), ld_dout, s.data_ptr(), ld_s, w, _ptr(dresidual), ld_r, ds.data_ptr(),
         _rows("ds", ds, shape, st, dev), _vector("dweight", dweight, (D,), dev), T, D, eps,
-        _DTYPES[dtype], _DTYPES[st], ws, wb, _stream(stream, dev)))
+        _DTYPES[dtype], _DTYPES[st], ws, wb, _stream(dev)))
     return ds, dweight
 
 
@@ -301,6 +334,9 @@ def lbi_ssm_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
     """The causal convolution of every channel with its W = 2 .. 4 taps weight [D, W] along the
     tokens of each sequence.  state_in, state_out [B, W - 1, D]: the tokens before each sequence
     and the last ones after it."""
+    if stream is not None:
+        return _aside(lbi_ssm_conv, stream, x, weight, bias, silu, offsets, sequences, state_in,
+                      state_out=state_out, slots=slots, out=out)
     shape, D, T, dtype, dev, ld_x, W, w, b = _conv_inputs(x, weight, bias)
     n = _batch(shape, offsets, sequences, dev)
     si, so, sp, ns = _states(state_in, state_out, slots, n, (W - 1, D), dtype, dev)
@@ -308,7 +344,7 @@ def lbi_ssm_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
         out = x.new_empty(shape)
     _check(load().lbi_ssm_conv(
         x.data_ptr(), ld_x, w, b, out.data_ptr(), _rows("out", out, shape, dtype, dev), si, so, sp,
-        ns, _ptr(offsets), T, n, D, W, int(silu), _DTYPES[dtype], _stream(stream, dev)))
+        ns, _ptr(offsets), T, n, D, W, int(silu), _DTYPES[dtype], _stream(dev)))
     return out
 
 
@@ -326,6 +362,9 @@ def lbi_ssm_conv_backward(x: torch.Tensor, weight: torch.Tensor, dout: torch.Ten
                           workspace: Optional[torch.Tensor] = None, stream=None):
     """(dx, dweight, dbias, dstate_in): dbias None without a bias, dstate_in None without
     state_in."""
+    if stream is not None:
+        return _aside(lbi_ssm_conv_backward, stream, x, weight, dout, bias, silu, offsets, sequences,
+                      state_in, dstate_out, dx=dx, workspace=workspace)
     shape, D, T, dtype, dev, ld_x, W, w, b = _conv_inputs(x, weight, bias)
     n = _batch(shape, offsets, sequences, dev)
     si, so, _, _ = _states(state_in, dstate_out, None, n, (W - 1, D), dtype, dev,
@@ -341,7 +380,7 @@ def lbi_ssm_conv_backward(x: torch.Tensor, weight: torch.Tensor, dout: torch.Ten
     _check(load().lbi_ssm_conv_backward(
         x.data_ptr(), ld_x, w, b, dout.data_ptr(), ld_dout, si, so, dx.data_ptr(),
         _rows("dx", dx, shape, dtype, dev), dweight.data_ptr(), _ptr(dbias), _ptr(dstate_in),
-        _ptr(offsets), T, n, D, W, int(silu), _DTYPES[dtype], ws, wb, _stream(stream, dev)))
+        _ptr(offsets), T, n, D, W, int(silu), _DTYPES[dtype], ws, wb, _stream(dev)))
     return dx, dweight, dbias, dstate_in
 
 
@@ -350,6 +389,9 @@ def lbi_ssm_conv_step(x: torch.Tensor, weight: torch.Tensor, state_in: torch.Ten
                       silu: bool = True, slots: Optional[torch.Tensor] = None,
                       out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """One token for each of n sequences, x [n, D]; state_out may be state_in."""
+    if stream is not None:
+        return _aside(lbi_ssm_conv_step, stream, x, weight, state_in, state_out, bias, silu, slots,
+                      out=out)
     shape, D, n, dtype, dev, ld_x, W, w, b = _conv_inputs(x, weight, bias)
     if len(shape) != 2:
         raise ValueError("x must be [n, D]")
@@ -358,7 +400,7 @@ def lbi_ssm_conv_step(x: torch.Tensor, weight: torch.Tensor, state_in: torch.Ten
         out = x.new_empty(shape)
     _check(load().lbi_ssm_conv_step(
         x.data_ptr(), ld_x, w, b, out.data_ptr(), _rows("out", out, shape, dtype, dev), si, so, sp,
-        ns, n, D, W, int(silu), _DTYPES[dtype], _stream(stream, dev)))
+        ns, n, D, W, int(silu), _DTYPES[dtype], _stream(dev)))
     return out
 
 
@@ -414,6 +456,10 @@ def lbi_ssm_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch
     """The selective scan of u under the steps softplus(delta + delta_bias), A [D, N] and the
     tokens' B, C [..., G, N] (or [..., N]), gated by silu(z).  state_in, state_out [B, D, N]
     float32: the states before and after each sequence; they may be the same tensor."""
+    if stream is not None:
+        return _aside(lbi_ssm_scan, stream, u, delta, A, B, C, skip, z, delta_bias, softplus,
+                      offsets, sequences, state_in, state_out=state_out, slots=slots, out=out,
+                      workspace=workspace)
     si, shape, dtype, dev = _scan_inputs(u, delta, A, B, C, skip, z, delta_bias, softplus, offsets,
                                          sequences, None)
     si.state_in, so, sp, ns = _states(state_in, state_out, slots, si.sequences, (si.D, si.N),
@@ -426,7 +472,7 @@ def lbi_ssm_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch
     workspace, w, wb = _scratch(need, workspace, dev)
     _check(lib.lbi_ssm_scan(
         ctypes.byref(si), out.data_ptr(), _rows("out", out, shape, dtype, dev), so, sp, ns, w, wb,
-        _stream(stream, dev)))
+        _stream(dev)))
     return out
 
 
@@ -448,6 +494,10 @@ def lbi_ssm_scan_backward(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor,
                           workspace: Optional[torch.Tensor] = None, stream=None) -> dict:
     """The gradients by input: "u", "delta", "A", "B", "C", "skip", "z", "delta_bias" and
     "state_in", None where the input is.  ``outputs``: tensors to write some of them to."""
+    if stream is not None:
+        return _aside(lbi_ssm_scan_backward, stream, u, delta, A, B, C, dout, skip, z, delta_bias,
+                      softplus, offsets, sequences, state_in, dstate_out, outputs=outputs,
+                      workspace=workspace)
     si, shape, dtype, dev = _scan_inputs(u, delta, A, B, C, skip, z, delta_bias, softplus, offsets,
                                          sequences, None)
     si.state_in, so, _, _ = _states(state_in, dstate_out, None, si.sequences, (si.D, si.N),
@@ -480,7 +530,7 @@ def lbi_ssm_scan_backward(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor,
                                                      int(offsets is not None))
     workspace, w, wb = _scratch(need, workspace, dev)
     _check(lib.lbi_ssm_scan_backward(ctypes.byref(si), dout.data_ptr(), ld_dout, so,
-                                     ctypes.byref(sg), w, wb, _stream(stream, dev)))
+                                     ctypes.byref(sg), w, wb, _stream(dev)))
     return g
 
 
@@ -491,6 +541,9 @@ def lbi_ssm_scan_step(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: 
                       slots: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                       stream=None) -> torch.Tensor:
     """One token for each of n sequences, u [n, D]; state_out may be state_in."""
+    if stream is not None:
+        return _aside(lbi_ssm_scan_step, stream, u, delta, A, B, C, state_in, state_out, skip, z,
+                      delta_bias, softplus, slots, out=out)
     if u.dim() != 2:
         raise ValueError("u must be [n, D]")
     si, shape, dtype, dev = _scan_inputs(u, delta, A, B, C, skip, z, delta_bias, softplus, None,
@@ -501,5 +554,5 @@ def lbi_ssm_scan_step(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: 
         out = u.new_empty(shape)
     _check(load().lbi_ssm_scan_step(
         ctypes.byref(si), out.data_ptr(), _rows("out", out, shape, dtype, dev), so, sp, ns,
-        _stream(stream, dev)))
+        _stream(dev)))
     return out

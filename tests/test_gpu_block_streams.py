@@ -1,0 +1,106 @@
+"""Calls of the region block on a stream that is not the current one, and on a device that is not
+(the GPU tests; the others need none)."""
+import pytest
+import torch
+
+from paper_2605_09204_amd import block
+
+gpu = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def calls():
+    """Every operator: (name, call with keyword arguments, workspace bytes)."""
+    g = torch.Generator()
+    g.manual_seed(21)
+    n = [900, 0, 5, 300]
+    T, S, D, N = sum(n), len(n), 200, 16
+
+    def r(*shape, dtype=torch.bfloat16):
+        return torch.randn(shape, generator=g).to(dtype).to(DEV)
+    f32 = torch.float32
+    off = torch.tensor([0, *n]).cumsum(0).to(DEV)
+    x, dy, w, cw, cb = r(T, D), r(T, D), r(D, dtype=f32), r(D, 4, dtype=f32), r(D, dtype=f32)
+    args = (x, r(T, D), -torch.rand(D, N, generator=g).to(DEV), r(T, 2, N), r(T, 2, N))
+    rest = {"skip": w, "z": r(T, D), "delta_bias": cb, "offsets": off, "state_in": r(S, D, N, dtype=f32)}
+    one = tuple(t if t.shape[0] == D else t[:S] for t in args)
+    cs, c_new, s_new = r(S, 3, D), r(S, 3, D), r(S, D, N, dtype=f32)
+    return [
+        ("norm", lambda **k: block.lbi_rms_norm(x, w, dy, **k), 0),
+        ("norm q8", lambda **k: block.lbi_rms_norm_q8(x, w, dy, group=64, **k), 0),
+        ("norm backward", lambda **k: block.lbi_rms_norm_backward(dy, x, w, **k),
+         block.lbi_rms_norm_backward_workspace_bytes(T, D)),
+        ("conv", lambda **k: block.lbi_ssm_conv(x, cw, cb, offsets=off, state_in=cs, **k), 0),
+        ("conv backward", lambda **k: block.lbi_ssm_conv_backward(x, cw, dy, cb, offsets=off,
+                                                                  state_in=cs, **k),
+         block.lbi_ssm_conv_backward_workspace_bytes(T, D, 4)),
+        ("conv step", lambda **k: block.lbi_ssm_conv_step(x[:S], cw, cs, c_new, cb, **k), 0),
+        ("scan", lambda **k: block.lbi_ssm_scan(*args, **rest, **k),
+         block.lbi_ssm_scan_workspace_bytes(T, S, D, N, 2, True)),
+        ("scan backward", lambda **k: block.lbi_ssm_scan_backward(*args, dy, **rest, **k),
+         block.lbi_ssm_scan_backward_workspace_bytes(T, S, D, N, 2, True)),
+        ("scan step", lambda **k: block.lbi_ssm_scan_step(*one, rest["state_in"], s_new, **k), 0),
+    ]
+
+
+def tensors(results):
+    results = results.values() if isinstance(results, dict) else \
+        results if isinstance(results, tuple) else (results,)
+    return [t for t in results if t is not None]
+
+
+def bits(t):
+    return t.contiguous().view(torch.uint8).clone()
+
+
+@gpu
+@pytest.mark.parametrize("handle", [False, True])
+def test_memory_of_a_call_on_another_stream(handle):
+    """The other stream is busy when the call comes, so its kernels run after the call has returned:
+    what the current stream allocates and fills meanwhile must not be the call's memory, and what
+    the call allocates must not be memory that the current stream is still filling."""
+    every = calls()
+    want = [[bits(t) for t in tensors(f())] for _, f, _ in every]
+    side = torch.cuda.Stream()
+    busy = torch.zeros(1 << 26, device=DEV)
+    assert sum(need > 0 for _, _, need in every) == 4
+    for (name, f, need), w in zip(every, want):
+        print(f"[streams] {name}, workspace of {need} bytes", flush=True)
+        sizes = sorted({need, *(t.numel() for t in w)} - {0})
+        torch.cuda.synchronize()
+        # blocks of these sizes lie free, and the current stream still writes to them
+        for _ in range(40):
+            busy.add_(1.0)
+        for size in sizes:
+            for _ in range(2):
+                torch.empty(size, dtype=torch.uint8, device=DEV).fill_(170)
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                busy.add_(1.0)
+        results = f(stream=side.cuda_stream if handle else side)
+        junk = [torch.empty(size, dtype=torch.uint8, device=DEV).fill_(85)
+                for size in sizes for _ in range(3)]
+        torch.cuda.synchronize()
+        got = tensors(results)
+        assert len(got) == len(w)
+        for a, b in zip(got, w):
+            assert torch.equal(bits(a), b), name
+        assert all((j == 85).all() for j in junk), f"{name} wrote to memory of the current stream"
+
+
+@gpu
+def test_the_callers_stream_stays_current():
+    side = torch.cuda.Stream()
+    x, w = torch.ones(4, 8, device=DEV), torch.ones(8, device=DEV)
+    before = torch.cuda.current_stream()
+    block.lbi_rms_norm(x, w, stream=side)
+    with pytest.raises(ValueError):
+        block.lbi_rms_norm(x, w[:4], stream=side)
+    assert torch.cuda.current_stream() == before
+    torch.cuda.synchronize()
+
+
+def test_tensors_off_the_gpu_are_refused_with_a_stream_too():
+    x = torch.ones(4, 8)
+    with pytest.raises(ValueError):
+        block.lbi_rms_norm(x, torch.ones(8), stream=7)
