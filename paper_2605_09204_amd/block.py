@@ -183,6 +183,8 @@ def _scratch(need: int, workspace, dev: int):
         if need == 0:
             return None, None, 0
         workspace = torch.empty((need,), dtype=torch.uint8, device=f"cuda:{dev}")
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on cuda:{dev}")
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 

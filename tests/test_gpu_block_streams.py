@@ -104,3 +104,21 @@ def test_tensors_off_the_gpu_are_refused_with_a_stream_too():
     x = torch.ones(4, 8)
     with pytest.raises(ValueError):
         block.lbi_rms_norm(x, torch.ones(8), stream=7)
+
+
+def test_a_workspace_off_the_gpu_is_refused():
+    for need in (0, 16):
+        with pytest.raises(ValueError):
+            block._scratch(need, torch.empty(256, dtype=torch.uint8), 0)
+
+
+@gpu
+def test_a_workspace_with_gaps_is_refused():
+    """What lies between its values is not its own."""
+    x, w = torch.ones(6, 8, device=DEV), torch.ones(8, device=DEV)
+    need = block.lbi_rms_norm_backward_workspace_bytes(6, 8)
+    with pytest.raises(ValueError):
+        block.lbi_rms_norm_backward(x, x, w, workspace=torch.empty(2 * need, dtype=torch.uint8,
+                                                                  device=DEV)[::2])
+    block.lbi_rms_norm_backward(x, x, w, workspace=torch.empty(need, dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()
