@@ -196,6 +196,19 @@ def _stream(dev: int) -> int:
     return _raw_stream(dev) if _raw_stream is not None else _stream_ptr(None, torch.device("cuda", dev))
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _run(dev: int, entry, *args):
+    """Calls an entry point with the tensors' device current: the default stream's handle is the same
+    for every device."""
+    if _current_device() == dev:
+        _check(entry(*args))
+    else:
+        with torch.cuda.device(dev):
+            _check(entry(*args))
+
+
 def _aside(call, stream, x, *args, **outputs):
     """The call on ``stream``, made the current one: what the call allocates then comes from that
     stream's memory, in its order.  Results are recorded on the caller's stream, where they may be
@@ -249,10 +262,10 @@ def lbi_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
         x, weight, residual, residual_out)
     if out is None:
         out = x.new_empty(shape)
-    _check(load().lbi_rms_norm(
-        x.data_ptr(), ld_x, _ptr(residual), ld_r, w, out.data_ptr(),
-        _rows("out", out, shape, dtype, dev), _ptr(residual_out), ld_o, T, D, eps,
-        _DTYPES[dtype], rdt, _stream(dev)))
+    _run(dev, load().lbi_rms_norm,
+         x.data_ptr(), ld_x, _ptr(residual), ld_r, w, out.data_ptr(),
+         _rows("out", out, shape, dtype, dev), _ptr(residual_out), ld_o, T, D, eps,
+         _DTYPES[dtype], rdt, _stream(dev))
     return out, residual_out
 
 
@@ -275,11 +288,11 @@ def lbi_rms_norm_q8(x: torch.Tensor, weight: torch.Tensor,
         q = x.new_empty(shape, dtype=_Q8_TYPES[format])
     if scales is None:
         scales = x.new_empty(groups, dtype=torch.float32)
-    _check(load().lbi_rms_norm_q8(
-        x.data_ptr(), ld_x, _ptr(residual), ld_r, w, q.data_ptr(),
-        _rows("q", q, shape, _Q8_TYPES[format], dev), _vector("scales", scales, groups, dev),
-        _ptr(residual_out), ld_o, T, D, eps, group, format, _DTYPES[dtype], rdt,
-        _stream(dev)))
+    _run(dev, load().lbi_rms_norm_q8,
+         x.data_ptr(), ld_x, _ptr(residual), ld_r, w, q.data_ptr(),
+         _rows("q", q, shape, _Q8_TYPES[format], dev), _vector("scales", scales, groups, dev),
+         _ptr(residual_out), ld_o, T, D, eps, group, format, _DTYPES[dtype], rdt,
+         _stream(dev))
     return q, scales, residual_out
 
 
@@ -309,10 +322,10 @@ def lbi_rms_norm_backward(dout: torch.Tensor, s: torch.Tensor, weight: torch.Ten
     if dweight is None:
         dweight = weight.new_empty((D,))
     workspace, ws, wb = _scratch(load().lbi_rms_norm_backward_workspace_bytes(T, D), workspace, dev)
-    _check(load().lbi_rms_norm_backward(
-        dout.data_ptr(), ld_dout, s.data_ptr(), ld_s, w, _ptr(dresidual), ld_r, ds.data_ptr(),
-        _rows("ds", ds, shape, st, dev), _vector("dweight", dweight, (D,), dev), T, D, eps,
-        _DTYPES[dtype], _DTYPES[st], ws, wb, _stream(dev)))
+    _run(dev, load().lbi_rms_norm_backward,
+         dout.data_ptr(), ld_dout, s.data_ptr(), ld_s, w, _ptr(dresidual), ld_r, ds.data_ptr(),
+         _rows("ds", ds, shape, st, dev), _vector("dweight", dweight, (D,), dev), T, D, eps,
+         _DTYPES[dtype], _DTYPES[st], ws, wb, _stream(dev))
     return ds, dweight
 
 
@@ -344,9 +357,9 @@ def lbi_ssm_conv(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Ten
     si, so, sp, ns = _states(state_in, state_out, slots, n, (W - 1, D), dtype, dev)
     if out is None:
         out = x.new_empty(shape)
-    _check(load().lbi_ssm_conv(
-        x.data_ptr(), ld_x, w, b, out.data_ptr(), _rows("out", out, shape, dtype, dev), si, so, sp,
-        ns, _ptr(offsets), T, n, D, W, int(silu), _DTYPES[dtype], _stream(dev)))
+    _run(dev, load().lbi_ssm_conv,
+         x.data_ptr(), ld_x, w, b, out.data_ptr(), _rows("out", out, shape, dtype, dev), si, so, sp,
+         ns, _ptr(offsets), T, n, D, W, int(silu), _DTYPES[dtype], _stream(dev))
     return out
 
 
@@ -379,10 +392,10 @@ def lbi_ssm_conv_backward(x: torch.Tensor, weight: torch.Tensor, dout: torch.Ten
     dstate_in = None if state_in is None else torch.empty_like(state_in)
     workspace, ws, wb = _scratch(load().lbi_ssm_conv_backward_workspace_bytes(T, D, W), workspace,
                                  dev)
-    _check(load().lbi_ssm_conv_backward(
-        x.data_ptr(), ld_x, w, b, dout.data_ptr(), ld_dout, si, so, dx.data_ptr(),
-        _rows("dx", dx, shape, dtype, dev), dweight.data_ptr(), _ptr(dbias), _ptr(dstate_in),
-        _ptr(offsets), T, n, D, W, int(silu), _DTYPES[dtype], ws, wb, _stream(dev)))
+    _run(dev, load().lbi_ssm_conv_backward,
+         x.data_ptr(), ld_x, w, b, dout.data_ptr(), ld_dout, si, so, dx.data_ptr(),
+         _rows("dx", dx, shape, dtype, dev), dweight.data_ptr(), _ptr(dbias), _ptr(dstate_in),
+         _ptr(offsets), T, n, D, W, int(silu), _DTYPES[dtype], ws, wb, _stream(dev))
     return dx, dweight, dbias, dstate_in
 
 
@@ -400,9 +413,9 @@ def lbi_ssm_conv_step(x: torch.Tensor, weight: torch.Tensor, state_in: torch.Ten
     si, so, sp, ns = _states(state_in, state_out, slots, n, (W - 1, D), dtype, dev)
     if out is None:
         out = x.new_empty(shape)
-    _check(load().lbi_ssm_conv_step(
-        x.data_ptr(), ld_x, w, b, out.data_ptr(), _rows("out", out, shape, dtype, dev), si, so, sp,
-        ns, n, D, W, int(silu), _DTYPES[dtype], _stream(dev)))
+    _run(dev, load().lbi_ssm_conv_step,
+         x.data_ptr(), ld_x, w, b, out.data_ptr(), _rows("out", out, shape, dtype, dev), si, so, sp,
+         ns, n, D, W, int(silu), _DTYPES[dtype], _stream(dev))
     return out
 
 
@@ -472,9 +485,9 @@ def lbi_ssm_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: torch
     need = lib.lbi_ssm_scan_workspace_bytes(si.T, si.sequences, si.D, si.N, si.G,
                                             int(offsets is not None))
     workspace, w, wb = _scratch(need, workspace, dev)
-    _check(lib.lbi_ssm_scan(
-        ctypes.byref(si), out.data_ptr(), _rows("out", out, shape, dtype, dev), so, sp, ns, w, wb,
-        _stream(dev)))
+    _run(dev, lib.lbi_ssm_scan,
+         ctypes.byref(si), out.data_ptr(), _rows("out", out, shape, dtype, dev), so, sp, ns, w, wb,
+         _stream(dev))
     return out
 
 
@@ -531,8 +544,8 @@ def lbi_ssm_scan_backward(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor,
     need = lib.lbi_ssm_scan_backward_workspace_bytes(si.T, si.sequences, si.D, si.N, si.G,
                                                      int(offsets is not None))
     workspace, w, wb = _scratch(need, workspace, dev)
-    _check(lib.lbi_ssm_scan_backward(ctypes.byref(si), dout.data_ptr(), ld_dout, so,
-                                     ctypes.byref(sg), w, wb, _stream(dev)))
+    _run(dev, lib.lbi_ssm_scan_backward, ctypes.byref(si), dout.data_ptr(), ld_dout, so,
+         ctypes.byref(sg), w, wb, _stream(dev))
     return g
 
 
@@ -554,7 +567,7 @@ def lbi_ssm_scan_step(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, B: 
                                       torch.float32, dev)
     if out is None:
         out = u.new_empty(shape)
-    _check(load().lbi_ssm_scan_step(
-        ctypes.byref(si), out.data_ptr(), _rows("out", out, shape, dtype, dev), so, sp, ns,
-        _stream(dev)))
+    _run(dev, load().lbi_ssm_scan_step,
+         ctypes.byref(si), out.data_ptr(), _rows("out", out, shape, dtype, dev), so, sp, ns,
+         _stream(dev))
     return out

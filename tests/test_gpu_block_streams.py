@@ -122,3 +122,44 @@ def test_a_workspace_with_gaps_is_refused():
                                                                   device=DEV)[::2])
     block.lbi_rms_norm_backward(x, x, w, workspace=torch.empty(need, dtype=torch.uint8, device=DEV))
     torch.cuda.synchronize()
+
+
+def test_a_call_makes_its_device_current(monkeypatch):
+    """The default stream of every device has the same handle: the kernels go to the current device."""
+    entered = []
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            entered.append(self.index)
+
+        def __exit__(self, *exc):
+            entered.append("left")
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(block, "_current_device", lambda: 0)
+    block._run(0, lambda *a: entered.append(a) or 0, 3)
+    assert entered == [(3,)]
+    entered.clear()
+    block._run(1, lambda *a: entered.append(a) or 0, 4, 5)
+    assert entered == [1, (4, 5), "left"]
+    entered.clear()
+    with pytest.raises(block.binding.LbiError):
+        block._run(1, lambda: 2)
+    assert entered == [1, "left"]
+    # no entry point is called past it
+    calls_of = open(block.__file__).read()
+    assert calls_of.count("_check(") == 2 and calls_of.count("    _run(dev, ") == 9
+
+
+@gpu
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two GPUs")
+def test_tensors_on_another_device():
+    x = torch.randn(6, 8)
+    want = block.lbi_rms_norm(x.to(DEV), torch.ones(8, device=DEV))[0].cpu()
+    with torch.cuda.device(0):
+        got = block.lbi_rms_norm(x.to("cuda:1"), torch.ones(8, device="cuda:1"))[0]
+        assert torch.cuda.current_device() == 0
+    assert got.device.index == 1 and torch.equal(got.cpu(), want)
