@@ -208,7 +208,7 @@ typedef struct {
     const float *state_in;   /* [sequences or n_slots][D][N], or NULL (zeros) */
     const int64_t *offsets;  /* [sequences + 1] DEVICE, or NULL               */
     int64_t T;               /* tokens of all sequences                       */
-    int64_t sequences;
+    int64_t sequences;       /* fewer than 2^32                               */
     int32_t D;               /* channels                                      */
     int32_t N;               /* states of a channel, 1 .. LBI_SSM_MAX_N       */
     int32_t G;               /* groups: channels g D/G .. share B and C; G

@@ -310,6 +310,20 @@ __device__ __forceinline__ int64_t state_row(const int32_t *slots, int32_t n_slo
     return s >= 0 && s < n_slots ? s : -1;
 }
 
+// Rows of `cols` workgroups of 256 in as many launches as they need: launch(first row, workgroups).
+template <typename F> hipError_t in_launches(int64_t rows, int64_t cols, F &&launch)
+{
+    const int64_t per = kMostGroups / cols;
+    for (int64_t first = 0; first < rows; first += per) {
+        const int64_t n = rows - first < per ? rows - first : per;
+        launch(first, dim3((unsigned)(n * cols)));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+    }
+    return hipSuccess;
+}
+
 // store(c, the sum over r < rows of partial[r * pitch + c]) for c < cols, in a
 // fixed order.  16 row groups x 64 columns a workgroup, so that a few hundred
 // rows are a few dozen loads deep.

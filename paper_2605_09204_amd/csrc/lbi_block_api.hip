@@ -10,7 +10,6 @@ namespace {
 
 constexpr int64_t kMostRows = (int64_t)1 << 40;  // of a token or state tensor
 constexpr int64_t kMostValues = (int64_t)1 << 46;
-constexpr int64_t kMostGroups = (int64_t)1 << 31;  // workgroups of a launch, exclusive
 
 size_t size_of(lbi_dtype dt) { return dt == LBI_F32 ? 4 : 2; }
 bool known(lbi_dtype dt) { return dt == LBI_F32 || dt == LBI_BF16; }
@@ -181,7 +180,7 @@ bool too_wide(std::initializer_list<int64_t> strides)
     return false;
 }
 
-bool too_many_groups(const SsmCut &c) { return c.ranges > (kMostGroups - 1) / c.tiles; }
+bool too_many_ranges(const SsmCut &c) { return c.ranges > UINT32_MAX; }
 
 size_t scan_layout(SsmArgs &a, void *workspace)
 {
@@ -397,8 +396,7 @@ lbi_status lbi_ssm_conv_step(const void *x, int64_t ld_x, const float *weight, c
 {
     if (!known(dt))
         return LBI_ERR_DTYPE;
-    if (bad_conv_shape(n, n, D, W, true) || (slots && n_slots < 0) ||
-        n > (kMostGroups - 1) * 256 / ((D + 7) / 8))
+    if (bad_conv_shape(n, n, D, W, true) || (slots && n_slots < 0))
         return LBI_ERR_SHAPE;
     if (n == 0)
         return LBI_OK;
@@ -454,7 +452,7 @@ lbi_status lbi_ssm_scan(const lbi_ssm_inputs *in, void *y, int64_t ld_y, float *
     a.state_out = state_out;
     a.slots = slots; a.n_slots = n_slots;
     a.cut = ssm_forward_cut(*in, in->offsets != nullptr);
-    if (too_many_groups(a.cut) || too_wide({in->ld_u, in->ld_delta, in->z ? in->ld_z : 0, in->ld_B,
+    if (too_many_ranges(a.cut) || too_wide({in->ld_u, in->ld_delta, in->z ? in->ld_z : 0, in->ld_B,
                                             in->ld_C, ld_y}))
         return LBI_ERR_SHAPE;
     const size_t need = scan_layout(a, workspace);
@@ -526,7 +524,7 @@ lbi_status lbi_ssm_scan_backward(const lbi_ssm_inputs *in, const void *dy, int64
         a.out.dz = nullptr;
     a.cut = ssm_backward_cut(*in, in->offsets != nullptr);
     const size_t need = backward_layout(a, workspace);
-    if (too_many_groups(a.cut) ||
+    if (too_many_ranges(a.cut) ||
         too_wide({in->ld_u, in->ld_delta, in->z ? in->ld_z : 0, in->ld_B, in->ld_C, ld_dy,
                   grads->ld_du, grads->ld_ddelta, in->z ? grads->ld_dz : 0, grads->ld_dB,
                   grads->ld_dC}))

@@ -10,6 +10,10 @@
 
 namespace lbi {
 
+// Workgroups of 256 in a launch, whose work items are fewer than 2^32: more would be refused, or
+// their number taken modulo 2^32.
+constexpr int64_t kMostGroups = (1 << 24) - 1;
+
 // ---- norm --------------------------------------------------------------------
 
 struct NormArgs {
@@ -71,6 +75,7 @@ struct SsmCut {
     int32_t per_sequence;
     int32_t tiles;  // workgroups along the channels, over all groups
     bool joined;    // states pass between ranges
+    uint32_t first; // the range that a launch begins with
 };
 SsmCut ssm_cut(int64_t T, int64_t sequences, int32_t D, int32_t G, bool ragged, double again,
                double launches);

@@ -25,7 +25,8 @@ template <typename T> constexpr int backward_piece_rows() { return 32 / sizeof(T
 // two), runs beside them in a workgroup of 256, and tokens a run.
 struct Cut {
     int lanes, runs, tokens;
-    int64_t row_blocks, col_blocks;
+    int64_t row_blocks;
+    int32_t col_blocks;
 };
 Cut cut_of(int64_t T, int32_t D, int V, int most)
 {
@@ -38,7 +39,8 @@ Cut cut_of(int64_t T, int32_t D, int V, int most)
         tokens *= 2;
     const int runs = 256 / lanes;
     const int64_t per = (int64_t)runs * tokens;
-    return {lanes, runs, tokens, (T + per - 1) / per, (vec + lanes - 1) / lanes};
+    return {lanes, runs, tokens, (T + per - 1) / per,
+            (int32_t)((vec + lanes - 1) / lanes)};
 }
 // Two channels a lane: the rows in flight and, in the gradient, its sums then leave
 // room for four wavefronts a SIMD, which the operations need.  16384 tokens, 1536 channels,
@@ -234,18 +236,18 @@ __device__ __forceinline__ void conv_run(const ConvArgs &a, const Sequences &q, 
     }
 }
 
-// Workgroups up to row_blocks convolve, those from row_blocks on write states.
+// Row blocks from `first` on: those below row_blocks convolve, the others write states.
 template <int W, typename T>
 __global__ __launch_bounds__(256) void conv_kernel(const ConvArgs a, const Cut c, int64_t first)
 {
     constexpr int V = kWidth;
     const Sequences q = {a.offsets, a.T, a.B, a.B > 0 ? a.T / a.B : 0};
-    const int64_t block_of = blockIdx.x / (unsigned)c.col_blocks;
-    const int col_block = (int)(blockIdx.x - block_of * c.col_blocks);
+    const unsigned row_of = blockIdx.x / (unsigned)c.col_blocks;
+    const int col_block = (int)(blockIdx.x - row_of * c.col_blocks);
     int d = (col_block * c.lanes + (int)threadIdx.x % c.lanes) * V, left = a.D - d;
     if (left <= 0)
         return;
-    const int64_t block = first + block_of;
+    const int64_t block = first + row_of;
     const int64_t run = block * c.runs + threadIdx.x / c.lanes;
     if (block >= c.row_blocks) {
         const int64_t s = run - c.row_blocks * c.runs;
@@ -267,11 +269,11 @@ __global__ __launch_bounds__(256) void conv_kernel(const ConvArgs a, const Cut c
 }
 
 template <int W, typename T>
-__global__ __launch_bounds__(256) void conv_step_kernel(const ConvArgs a)
+__global__ __launch_bounds__(256) void conv_step_kernel(const ConvArgs a, int64_t first)
 {
     constexpr int V = 16 / sizeof(T);
     const int64_t vec = (a.D + V - 1) / V;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t id = (first + blockIdx.x) * 256 + threadIdx.x;
     const int64_t row = id / vec;
     const int d = (int)(id - row * vec) * V, left = a.D - d;
     if (row >= a.T)
@@ -481,12 +483,14 @@ __device__ __forceinline__ void backward_edge(const ConvArgs &a, const Segment &
 }
 
 template <int W, typename T>
-__global__ __launch_bounds__(256) void conv_backward_kernel(const ConvArgs a, const Cut c)
+__global__ __launch_bounds__(256) void conv_backward_kernel(const ConvArgs a, const Cut c,
+                                                            int64_t first)
 {
     constexpr int V = kWidth;
     const Sequences q = {a.offsets, a.T, a.B, a.B > 0 ? a.T / a.B : 0};
-    const int64_t block_of = blockIdx.x / (unsigned)c.col_blocks;
-    const int col_block = (int)(blockIdx.x - block_of * c.col_blocks);
+    const unsigned row_of = blockIdx.x / (unsigned)c.col_blocks;
+    const int col_block = (int)(blockIdx.x - row_of * c.col_blocks);
+    const int64_t block_of = first + row_of;
     int d = (col_block * c.lanes + (int)threadIdx.x % c.lanes) * V, left = a.D - d;
     const int64_t run = block_of * c.runs + threadIdx.x / c.lanes;
     if (block_of >= c.row_blocks) {
@@ -591,24 +595,22 @@ template <typename T> hipError_t forward(const ConvArgs &a, hipStream_t stream)
     // In place, a state may be written only when every run has read it.
     const bool in_place = a.state_out && a.state_out == a.state_in;
     return by_taps(a.W, [&](auto w) {
-        const int64_t n = c.row_blocks + (in_place ? 0 : states);
-        if (n > 0)
-            conv_kernel<decltype(w)::value, T>
-                <<<dim3((unsigned)(n * c.col_blocks)), 256, 0, stream>>>(a, c, 0);
-        if (in_place && states > 0)
-            conv_kernel<decltype(w)::value, T>
-                <<<dim3((unsigned)(states * c.col_blocks)), 256, 0, stream>>>(a, c,
-                                                                                     c.row_blocks);
-        return hipGetLastError();
+        auto blocks = [&](int64_t from, int64_t n) {
+            return in_launches(n, c.col_blocks, [&](int64_t first, dim3 grid) {
+                conv_kernel<decltype(w)::value, T><<<grid, 256, 0, stream>>>(a, c, from + first);
+            });
+        };
+        const hipError_t e = blocks(0, c.row_blocks + (in_place ? 0 : states));
+        return e == hipSuccess && in_place ? blocks(c.row_blocks, states) : e;
     });
 }
 template <typename T> hipError_t step(const ConvArgs &a, hipStream_t stream)
 {
     const int64_t threads = a.T * ((a.D + 16 / sizeof(T) - 1) / (16 / sizeof(T)));
     return by_taps(a.W, [&](auto w) {
-        conv_step_kernel<decltype(w)::value, T>
-            <<<dim3((unsigned)((threads + 255) / 256)), 256, 0, stream>>>(a);
-        return hipGetLastError();
+        return in_launches((threads + 255) / 256, 1, [&](int64_t first, dim3 grid) {
+            conv_step_kernel<decltype(w)::value, T><<<grid, 256, 0, stream>>>(a, first);
+        });
     });
 }
 template <typename T> hipError_t backward(const ConvArgs &a, hipStream_t stream)
@@ -617,10 +619,9 @@ template <typename T> hipError_t backward(const ConvArgs &a, hipStream_t stream)
     const bool empty = a.state_out && (a.offsets || a.T == 0);  // empty sequences are possible
     const int64_t n = c.row_blocks + (empty ? (a.B + c.runs - 1) / c.runs : 0);
     return by_taps(a.W, [&](auto w) {
-        if (n > 0)
-            conv_backward_kernel<decltype(w)::value, T>
-                <<<dim3((unsigned)(n * c.col_blocks)), 256, 0, stream>>>(a, c);
-        return hipGetLastError();
+        return in_launches(n, c.col_blocks, [&](int64_t first, dim3 grid) {
+            conv_backward_kernel<decltype(w)::value, T><<<grid, 256, 0, stream>>>(a, c, first);
+        });
     });
 }
 

@@ -57,8 +57,9 @@ __global__ __launch_bounds__(256, NS <= 4 ? 4 : 2) void scan_kernel(const SsmArg
     __shared__ __align__(16) float ys[ENDS ? 1 : kTile][kPitch];
     const lbi_ssm_inputs &in = a.in;
     const Sequences q = ssm_sequences(in);
-    const int64_t r = blockIdx.x / (unsigned)a.cut.tiles;
-    const Tile tile = tile_of(in, (int)(blockIdx.x - r * a.cut.tiles));
+    const unsigned row_of = blockIdx.x / (unsigned)a.cut.tiles;
+    const int64_t r = row_of + a.cut.first;
+    const Tile tile = tile_of(in, (int)(blockIdx.x - row_of * a.cut.tiles));
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4;
     const int c = (tid >> 6) * 16 + (lane & 15);
     const int nn = c < tile.left ? in.N - g * NS : 0;  // states that this lane holds (at most NS)
@@ -301,19 +302,20 @@ __global__ __launch_bounds__(256) void scan_step_kernel(const SsmArgs a)
 
 template <typename T> hipError_t forward(const SsmArgs &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(a.cut.ranges * a.cut.tiles));
     return by_states(a.in.N, [&](auto ns) {
         constexpr int NS = decltype(ns)::value;
         if (a.cut.joined) {
-            scan_kernel<T, NS, true><<<grid, 256, 0, stream>>>(a);
-            hipError_t e = hipGetLastError();
+            hipError_t e = over_ranges(a, [&](const SsmArgs &b, dim3 grid) {
+                scan_kernel<T, NS, true><<<grid, 256, 0, stream>>>(b);
+            });
             if (e == hipSuccess)
                 e = launch_carry(a, stream);
             if (e != hipSuccess)
                 return e;
         }
-        scan_kernel<T, NS, false><<<grid, 256, 0, stream>>>(a);
-        return hipGetLastError();
+        return over_ranges(a, [&](const SsmArgs &b, dim3 grid) {
+            scan_kernel<T, NS, false><<<grid, 256, 0, stream>>>(b);
+        });
     });
 }
 
@@ -347,7 +349,7 @@ SsmCut ssm_cut(int64_t T, int64_t sequences, int32_t D, int32_t G, bool ragged, 
 {
     constexpr double START = 16;
     constexpr int64_t CUS = 256;
-    SsmCut c;
+    SsmCut c = {};
     c.tiles = G * ((D / G + kChannels - 1) / kChannels);
     const int64_t rows = ragged || sequences == 0 ? T : T / sequences;
     const int64_t many = ragged || sequences == 0 ? 1 : sequences;

@@ -290,6 +290,16 @@ inline hipError_t launch_carry(const SsmArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
+// launch(arguments, workgroups) for all ranges.
+template <typename F> hipError_t over_ranges(const SsmArgs &a, F &&launch)
+{
+    return in_launches(a.cut.ranges, a.cut.tiles, [&](int64_t first, dim3 grid) {
+        SsmArgs b = a;
+        b.cut.first = (uint32_t)first;
+        launch(b, grid);
+    });
+}
+
 // Calls f<NS>() for the states a lane holds.
 template <typename F> hipError_t by_states(int32_t N, F &&f)
 {

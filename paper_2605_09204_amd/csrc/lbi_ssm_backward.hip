@@ -49,8 +49,9 @@ __global__ __launch_bounds__(256, NS <= 2 ? 4 : (NS == 4 ? 3 : (NS == 8 ? 2 : 1)
     __shared__ float es[JOINED ? kSweep : 1][kChannels];
     const lbi_ssm_inputs &in = a.in;
     const Sequences q = ssm_sequences(in);
-    const int64_t r = blockIdx.x / (unsigned)a.cut.tiles;
-    const Tile tile = tile_of(in, (int)(blockIdx.x - r * a.cut.tiles));
+    const unsigned row_of = blockIdx.x / (unsigned)a.cut.tiles;
+    const int64_t r = row_of + a.cut.first;
+    const Tile tile = tile_of(in, (int)(blockIdx.x - row_of * a.cut.tiles));
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4;
     const int c = (tid >> 6) * 16 + (lane & 15);
     const int nn = c < tile.left ? in.N - g * NS : 0;
@@ -261,8 +262,9 @@ __global__ __launch_bounds__(256, waves_of<T>(NS)) void gradient_kernel(const Ss
     __shared__ __align__(16) float par[2][kChannels], sums[2][256 / LANES_V][kChannels];
     const lbi_ssm_inputs &in = a.in;
     const Sequences q = ssm_sequences(in);
-    const int64_t r = blockIdx.x / (unsigned)a.cut.tiles;
-    const Tile tile = tile_of(in, (int)(blockIdx.x - r * a.cut.tiles));
+    const unsigned row_of = blockIdx.x / (unsigned)a.cut.tiles;
+    const int64_t r = row_of + a.cut.first;
+    const Tile tile = tile_of(in, (int)(blockIdx.x - row_of * a.cut.tiles));
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, wave = tid >> 6;
     const int c = wave * 16 + (lane & 15);
     const int nn = c < tile.left ? in.N - g * NS : 0;
@@ -600,10 +602,10 @@ struct ToParameters {
 };
 
 // dB and dC from the channel tiles' sums, two float2 a thread and tile.
-template <typename T> __global__ __launch_bounds__(256) void sum_tiles_kernel(const SsmArgs a)
+template <typename T> __global__ __launch_bounds__(256) void sum_tiles_kernel(const SsmArgs a, int64_t first)
 {
     const int64_t gn = (int64_t)a.in.G * a.in.N, all = a.in.T * gn;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t i = (first + blockIdx.x) * 256 + threadIdx.x;
     if (i >= all)
         return;
     const int tiles = a.cut.tiles / a.in.G;
@@ -633,19 +635,19 @@ template <typename T> __global__ __launch_bounds__(256) void sum_tiles_kernel(co
 
 template <typename T, int NS, bool JOINED> hipError_t walks(const SsmArgs &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(a.cut.ranges * a.cut.tiles));
     hipError_t e = hipSuccess;
     // without ranges to join, marks are needed only past a sequence's first step
-    if (JOINED || a.in.offsets || a.in.T / a.in.sequences > step_of(NS)) {
-        sweep_kernel<T, NS, JOINED><<<grid, 256, 0, stream>>>(a);
-        e = hipGetLastError();
-    }
+    if (JOINED || a.in.offsets || a.in.T / a.in.sequences > step_of(NS))
+        e = over_ranges(a, [&](const SsmArgs &b, dim3 grid) {
+            sweep_kernel<T, NS, JOINED><<<grid, 256, 0, stream>>>(b);
+        });
     if (JOINED && e == hipSuccess)
         e = launch_carry(a, stream);
     if (e != hipSuccess)
         return e;
-    gradient_kernel<T, NS, JOINED><<<grid, 256, 0, stream>>>(a);
-    return hipGetLastError();
+    return over_ranges(a, [&](const SsmArgs &b, dim3 grid) {
+        gradient_kernel<T, NS, JOINED><<<grid, 256, 0, stream>>>(b);
+    });
 }
 
 template <typename T> hipError_t backward(const SsmArgs &a, hipStream_t stream)
@@ -660,8 +662,9 @@ template <typename T> hipError_t backward(const SsmArgs &a, hipStream_t stream)
         return e;
     const int64_t values = a.in.T * a.in.G * a.in.N;
     if (values > 0) {
-        sum_tiles_kernel<T><<<dim3((unsigned)((values + 255) / 256)), 256, 0, stream>>>(a);
-        e = hipGetLastError();
+        e = in_launches((values + 255) / 256, 1, [&](int64_t first, dim3 grid) {
+            sum_tiles_kernel<T><<<grid, 256, 0, stream>>>(a, first);
+        });
         if (e != hipSuccess)
             return e;
     }
