@@ -202,7 +202,10 @@ typedef struct {
     int64_t ld_B;
     const void *C;           /* [T][G][N] dt                                  */
     int64_t ld_C;
-    const float *A;          /* [D][N]; exp(D_t A) decays where A < 0         */
+    const float *A;          /* [D][N]; exp(D_t A) decays where A < 0.  A > 0:
+                              * states and outputs are as token by token; the
+                              * gradient of a state before tokens that together
+                              * grow it by 2^127 may be infinite or NaN       */
     const float *skip;       /* [D], or NULL (= 0)                            */
     const float *delta_bias; /* [D], or NULL (= 0)                            */
     const float *state_in;   /* [sequences or n_slots][D][N], or NULL (zeros) */

@@ -37,6 +37,26 @@ __device__ __forceinline__ float decay(float step, float A2)
     return __builtin_amdgcn_exp2f(fmaf(step, A2, 6e-9f));
 }
 
+// h 2^p, p = whole + part: the product over a range's decays (p = A2 sum D_t), also where 2^p alone
+// passes float32's range and h 2^p does not (A > 0, and h zero or small).
+__device__ __forceinline__ float power_parts(float p, int *whole)
+{
+    p = fminf(fmaxf(p, -1e5f), 1e5f);
+    const float w = rintf(p);
+    *whole = (int)w;
+    return __builtin_amdgcn_exp2f(p - w);
+}
+__device__ __forceinline__ float grown(float h, float part, int whole)
+{
+    return __builtin_amdgcn_ldexpf(h * part, whole);
+}
+__device__ __forceinline__ float grown(float h, float p)
+{
+    int whole;
+    const float part = power_parts(p, &whole);
+    return grown(h, part, whole);
+}
+
 // The steps D_t of V channels from delta + delta_bias.  (The choice stands outside
 // the loop: V chains of dependent operations at once.)
 template <int V> __device__ __forceinline__ void steps_of(bool use_softplus, float (&d)[V])
@@ -182,14 +202,14 @@ __device__ __forceinline__ float sum_states(const float (&v)[4])
 // the ranges that follow each other: one lane a channel and state.  Its time is trips to
 // memory, so each of WAVES wavefronts has the ends of DEEP consecutive ranges in flight;
 // the wavefronts exchange what their ranges do to a state that enters them (the end from zero, and
-// the decay), and each then walks its ranges again from the state that does enter.
+// the power of two that decays it), and each then walks its ranges again from the state that does enter.
 // The ranges of 32768 tokens, 12288 states: 7.4 us, one wavefront in batches of 32 ranges 15.4.
 // Up to 8 ranges one trip does, with one wavefront (5.5 us for 8 sequences of 24576 states).
 template <int DEEP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void carry_kernel(const SsmArgs a)
 {
     struct Map {
-        float end, decay;  // decay < 0: a sequence starts within, and what enters is dropped
+        float end, power;  // power NaN: a sequence starts within, and what enters is dropped
     };
     __shared__ Map maps[WAVES > 1 ? 2 : 1][WAVES > 1 ? WAVES : 1][64];
     const int lane = threadIdx.x % 64, wave = (int)uniform(threadIdx.x / 64);
@@ -216,7 +236,8 @@ __global__ __launch_bounds__(64 * WAVES) void carry_kernel(const SsmArgs a)
         const float *sums = a.sums + at * a.in.D + d;
         const uint64_t stop =
             __ballot(lane < mine && (a.flags[at + (lane < mine ? lane * one : 0)] & stops));
-        float e[DEEP], w[DEEP];
+        float e[DEEP], w[DEEP];  // ends; powers, then their parts
+        int n[DEEP];
         {
             const float *p = ends, *s = sums;
 #pragma unroll
@@ -227,21 +248,22 @@ __global__ __launch_bounds__(64 * WAVES) void carry_kernel(const SsmArgs a)
                 s += j + 1 < mine ? along : 0;
             }
         }
+        float power = 0.f;  // of all of them
 #pragma unroll
-        for (int j = 0; j < DEEP; ++j)
-            w[j] = __builtin_amdgcn_exp2f(A2 * w[j]);
+        for (int j = 0; j < DEEP; ++j) {
+            const float p = A2 * w[j];
+            power += j < mine ? p : 0.f;
+            w[j] = power_parts(p, &n[j]);
+        }
         if constexpr (WAVES > 1) {
-            Map m = {0.f, 1.f};
+            Map m = {0.f, stop ? __builtin_nanf("") : power};
 #pragma unroll
             for (int j = 0; j < DEEP; ++j) {
                 if (j < mine) {
                     const bool drop = stop >> j & 1;
-                    m.end = drop ? e[j] : fmaf(w[j], m.end, e[j]);
-                    m.decay *= w[j];
+                    m.end = drop ? e[j] : e[j] + grown(m.end, w[j], n[j]);
                 }
             }
-            if (stop)
-                m.decay = -1.f;
             maps[parity][wave][lane] = m;
             __syncthreads();
             float enters = cur;
@@ -250,13 +272,13 @@ __global__ __launch_bounds__(64 * WAVES) void carry_kernel(const SsmArgs a)
                 const Map o = maps[parity][v][lane];
                 if (v == wave)
                     enters = cur;
-                cur = o.decay < 0.f ? o.end : fmaf(o.decay, cur, o.end);
+                cur = o.power != o.power ? o.end : o.end + grown(cur, o.power);
             }
             parity ^= 1;  // the next maps go where nobody reads any more
 #pragma unroll
             for (int j = 0; j < DEEP; ++j) {
                 if (j < mine) {
-                    enters = stop >> j & 1 ? e[j] : fmaf(w[j], enters, e[j]);
+                    enters = stop >> j & 1 ? e[j] : e[j] + grown(enters, w[j], n[j]);
                     if (live)
                         *ends = enters;
                     ends += down;
@@ -266,7 +288,7 @@ __global__ __launch_bounds__(64 * WAVES) void carry_kernel(const SsmArgs a)
 #pragma unroll
             for (int j = 0; j < DEEP; ++j) {
                 if (j < mine) {
-                    cur = stop >> j & 1 ? e[j] : fmaf(w[j], cur, e[j]);
+                    cur = stop >> j & 1 ? e[j] : e[j] + grown(cur, w[j], n[j]);
                     if (live)
                         *ends = cur;
                     ends += down;

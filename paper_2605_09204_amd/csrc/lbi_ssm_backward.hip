@@ -418,9 +418,19 @@ __global__ __launch_bounds__(256, waves_of<T>(NS)) void gradient_kernel(const Ss
         for (int i = 0; i < NS; ++i)
             hs[0][i] = next_h[i];
         if (JOINED && seg.start < t0 && t > lo) {
+            bool far = false;  // a state of the wavefront grows by 2^127
 #pragma unroll
             for (int i = 0; i < NS; ++i)
-                hs[0][i] = fmaf(__builtin_amdgcn_exp2f(A2[i] * next_sum), entry[i], hs[0][i]);
+                far |= A2[i] * next_sum > 126.f;
+            if (__ballot(far)) {
+#pragma unroll
+                for (int i = 0; i < NS; ++i)
+                    hs[0][i] += grown(entry[i], A2[i] * next_sum);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NS; ++i)
+                    hs[0][i] = fmaf(__builtin_amdgcn_exp2f(A2[i] * next_sum), entry[i], hs[0][i]);
+            }
         }
         __syncthreads();
         const int64_t at = t, from = lo, seq = seg.seq;
