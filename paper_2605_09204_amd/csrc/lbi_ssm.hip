@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256, NS <= 4 ? 4 : 2) void scan_kernel(const SsmArg
     load_states<NS>(part_of(in.A, dn), nn, A2);
 #pragma unroll
     for (int i = 0; i < NS; ++i)
-        A2[i] *= kLog2e;
+        A2[i] = power_rate(A2[i]);
 
     // staging: a row and eight channels a thread, and E values of B and C
     const int row = tid >> 3, ch = (tid & 7) * 8, left = tile.left - ch;
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(const SsmArgs a)
         float y = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            h[i] = fmaf(decay(v, A2[i] * kLog2e), h[i], x * b[i]);
+            h[i] = fmaf(decay(v, power_rate(A2[i])), h[i], x * b[i]);
             y = fmaf(c[i], h[i], y);
         }
         if (row >= 0)

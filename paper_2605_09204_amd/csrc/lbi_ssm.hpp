@@ -27,7 +27,13 @@ __device__ __forceinline__ float softplus(float v)
     return fmaf(__builtin_amdgcn_logf(w), kLn2, e - (w - 1.f)) + fmaxf(v, 0.f);
 }
 
-// A token's decay exp(D_t A) = 2^p, p = D_t A2 with A2 = A log2(e).  The hardware's 2^p
+// A2 = A log2(e), kept finite: rows past a tile's last one have D_t = 0, and 0 (-inf) is NaN.
+__device__ __forceinline__ float power_rate(float A)
+{
+    const float A2 = A * kLog2e;
+    return A2 < -3.4e38f ? -3.4e38f : A2;
+}
+// A token's decay exp(D_t A) = 2^p, p = D_t A2.  The hardware's 2^p
 // is a little low on average where it matters, close below 1: by 0.11 units of the
 // last place for p in (-0.001, 0) and 0.07 in (-0.01, -0.001), and products of hundreds of
 // such decays carry that on (the gradient of A over 4600 tokens: 4e-6 off).  6e-9 added to p
@@ -223,7 +229,7 @@ __global__ __launch_bounds__(64 * WAVES) void carry_kernel(const SsmArgs a)
     const int64_t count = a.cut.per_sequence > 0 ? a.cut.per_sequence : a.cut.ranges;
     const int64_t first = (int64_t)blockIdx.y * count;
     const int32_t stops = reverse ? kEnds : kStarts;
-    const float A2 = a.in.A[i] * kLog2e;
+    const float A2 = power_rate(a.in.A[i]);
     const int64_t from = reverse ? first + count - 1 : first, one = reverse ? -1 : 1;
     const int64_t down = one * dN, along = one * a.in.D;  // to the next range
     float cur = 0.f;

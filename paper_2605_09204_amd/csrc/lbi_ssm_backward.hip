@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256, NS <= 2 ? 4 : (NS == 4 ? 3 : (NS == 8 ? 2 : 1)
     load_states<NS>(part_of(in.A, dn), nn, A2);
 #pragma unroll
     for (int i = 0; i < NS; ++i)
-        A2[i] *= kLog2e;
+        A2[i] = power_rate(A2[i]);
     // what the first sequence's tokens send to the gradient at the range's start
     float head[NS], way[NS];  // way: the decay from the start
 #pragma unroll
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(256, waves_of<T>(NS)) void gradient_kernel(const Ss
     load_states<NS>(part_of(in.A, dn), nn, A2);
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-        A2[i] *= kLog2e;
+        A2[i] = power_rate(A2[i]);
         dA[i] = 0.f;
     }
 

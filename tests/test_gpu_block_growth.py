@@ -1,4 +1,5 @@
-"""Channels whose states grow (A > 0) in scans that are cut into ranges (needs a GPU).
+"""Channels whose states grow (A > 0), or forget everything at each token (A = -inf), in scans that
+are cut into ranges (needs a GPU).
 
 Tolerances as in test_gpu_block.py: 1e-5 of the result's norm, each channel by itself here.
 """
@@ -61,3 +62,28 @@ def test_states_that_grow(T, step, ragged):
     close(got["u"][:live], want["u"], "u", 0)
     assert (got["u"][live:] == 0).all()
     close(got["state_in"], want["state_in"], "state_in", (0, 2))
+
+@pytest.mark.parametrize("n", [[3], [37, 5, 1, 8, 66], [1500]])
+def test_states_that_forget(n):
+    """A = -inf: h is the token's own part.  (Rows past a sequence's end change nothing.)"""
+    D, N, T = 2, 3, sum(n)
+    g = torch.Generator()
+    g.manual_seed(T)
+
+    def r(*shape):
+        return torch.randn(shape, generator=g).to(DEV)
+    A = torch.tensor([[-1.0, -float("inf"), -2.0], [-float("inf")] * 3]).to(DEV)
+    s = {"u": r(T, D), "delta": r(T, D), "A": A, "B": r(T, 1, N), "C": r(T, 1, N),
+         "state_in": r(len(n), D, N)}
+    off = torch.tensor([0, *n]).cumsum(0).to(DEV)
+    last = torch.empty(len(n), D, N, device=DEV)
+    y = block.lbi_ssm_scan(**s, offsets=off, state_out=last)
+    want, want_last = ref.scan(s, n)
+    close(y, want, "y", 0)
+    close(last, want_last, "state_out", (0, 2))
+    step = torch.empty(len(n), D, N, device=DEV)
+    one = {k: v[:len(n)] if k in ("u", "delta", "B", "C") else v for k, v in s.items() if k != "state_in"}
+    y = block.lbi_ssm_scan_step(**one, state_in=s["state_in"], state_out=step)
+    want, want_last = ref.scan({**one, "state_in": s["state_in"]}, [1] * len(n))
+    close(y, want, "step y", 0)
+    close(step, want_last, "step states", (0, 2))
