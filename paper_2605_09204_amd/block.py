@@ -100,6 +100,13 @@ def load() -> ctypes.CDLL:
 # The checks below are what a small call spends most of its host time on: they compare with `is`
 # and by device index, and take shapes and strides once.
 
+def _int32(name: str, value: int) -> int:
+    """The library takes it in 32 bits, and a larger one would be cut to them."""
+    if not -(1 << 31) <= value < 1 << 31:
+        raise ValueError(f"{name} is out of range: {value}")
+    return value
+
+
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
@@ -143,6 +150,7 @@ def _tokens(name: str, x: torch.Tensor):
     if len(shape) not in (2, 3) or not x.is_cuda:
         raise ValueError(f"{name} must be a [T, D] or [B, L, D] GPU tensor")
     T = shape[0] if len(shape) == 2 else shape[0] * shape[1]
+    _int32(f"{name}'s row", shape[-1])
     return shape, T, dtype, x.get_device(), _row_stride(name, shape, x.stride())
 
 
@@ -157,6 +165,8 @@ def _batch(shape, offsets, sequences, dev: int) -> int:
         _vector("offsets", offsets, (n + 1,), dev, torch.int64)
     else:
         n = shape[0] if len(shape) == 3 else (1 if sequences is None else int(sequences))
+        if n >> 62 not in (0, -1):
+            raise ValueError(f"sequences is out of range: {n}")
     if sequences is not None and int(sequences) != n:
         raise ValueError(f"sequences is {sequences}, the tensors hold {n}")
     return n
@@ -169,7 +179,7 @@ def _states(state_in, state_out, slots, n: int, tail, dtype, dev: int, names=("s
     rows, ptrs = n, []
     if slots is not None:
         some = state_in if state_in is not None else state_out
-        rows = 0 if some is None else some.shape[0]
+        rows = 0 if some is None else _int32("the states' rows", some.shape[0])
     for name, t in zip(names, (state_in, state_out)):
         ptrs.append(_vector(name, t, (rows, *tail), dev, dtype))
     if slots is None:
@@ -283,7 +293,7 @@ def lbi_rms_norm_q8(x: torch.Tensor, weight: torch.Tensor,
         x, weight, residual, residual_out)
     if format not in _Q8_TYPES:
         raise ValueError(f"format must be LBI_Q8_E4M3 or LBI_Q8_INT8, got {format}")
-    groups = (*shape[:-1], -(-D // group) if group > 0 else 1)
+    groups = (*shape[:-1], -(-D // group) if _int32("group", group) > 0 else 1)
     if q is None:
         q = x.new_empty(shape, dtype=_Q8_TYPES[format])
     if scales is None:
@@ -336,7 +346,7 @@ def _conv_inputs(x, weight, bias):
     D = shape[-1]
     if weight.dim() != 2:
         raise ValueError("weight must be [D, W]")
-    W = weight.shape[1]
+    W = _int32("W", weight.shape[1])
     return (shape, D, T, dtype, dev, ld_x, W, _vector("weight", weight, (D, W), dev),
             _vector("bias", bias, (D,), dev))
 
@@ -431,7 +441,7 @@ def _groups(name, t, lead, N: int, dtype, dev: int):
     G = shape[k] if len(shape) > k + 1 else 1
     if (N > 1 and stride[-1] != 1) or (G > 1 and stride[-2] != N):
         raise ValueError(f"{name}: a token's values must lie side by side")
-    return _row_stride(name, (*lead, G * N), (*stride[:k], 1)), G
+    return _row_stride(name, (*lead, G * N), (*stride[:k], 1)), _int32("G", G)
 
 
 def _scan_inputs(u, delta, A, B, C, skip, z, delta_bias, softplus, offsets, sequences, state_in):
@@ -440,7 +450,7 @@ def _scan_inputs(u, delta, A, B, C, skip, z, delta_bias, softplus, offsets, sequ
     D, lead = shape[-1], shape[:-1]
     if A.dim() != 2:
         raise ValueError("A must be [D, N]")
-    N = A.shape[1]
+    N = _int32("N", A.shape[1])
     ld_B, G = _groups("B", B, lead, N, dtype, dev)
     ld_C, G2 = _groups("C", C, lead, N, dtype, dev)
     if G != G2:

@@ -3,6 +3,7 @@ is used."""
 import os
 
 import pytest
+import torch
 
 from paper_2605_09204_amd import binding, block
 from test_block_abi import SHAPE, scan
@@ -27,3 +28,16 @@ def test_build_refuses_scratch():
             "remark:     VGPRs Spill: 0 [-R]\nremark: Function Name: c [-R]\n"
             "remark:     ScratchSize [bytes/lane]: 8 [-R]\nremark:     VGPRs Spill: 2 [-R]\n")
     assert build.spills(text) == ["b", "c"]
+
+
+def test_sizes_that_32_bits_do_not_hold():
+    """They were cut to 32 bits: a group of 2^32 + 128 features wrote scales for groups of 128."""
+    assert block._int32("n", (1 << 31) - 1) == (1 << 31) - 1 and block._int32("n", -5) == -5
+    for size in (1 << 31, (1 << 32) + 128, -(1 << 31) - 1):
+        with pytest.raises(ValueError):
+            block._int32("n", size)
+    with pytest.raises(ValueError):
+        block._batch((6, 8), None, (1 << 64) + 1, 0)
+    meta = torch.empty((1 << 32) + 2, 2, 8, device="meta")
+    with pytest.raises(ValueError, match="out of range"):
+        block._states(meta, None, torch.empty(1, dtype=torch.int32), 1, (2, 8), torch.float32, 0)

@@ -93,3 +93,11 @@ def test_values_against_64_bits(T, D, dtype, stream, fmt):
         else:
             bound = sc * 0.5
         assert (err <= bound * (1 + 1e-4) + 1e-30).all(), (err / bound).max()
+
+
+def test_a_group_that_32_bits_do_not_hold_is_refused():
+    x, w = torch.zeros(6, 256, device=DEV), torch.ones(256, device=DEV)
+    for group in (1 << 32, (1 << 32) + 128, -(1 << 32) + 32):
+        with pytest.raises(ValueError):
+            block.lbi_rms_norm_q8(x, w, group=group)
+    torch.cuda.synchronize()
