@@ -529,8 +529,11 @@ def lbi_ssm_scan_backward(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor,
                                     torch.float32, dev, ("state_in", "dstate_out"))
     ld_dout = _rows("dout", dout, shape, dtype, dev)
     g = {} if outputs is None else dict(outputs)
-    for name, t in (("u", u), ("delta", delta), ("A", A), ("B", B), ("C", C), ("skip", skip),
-                    ("z", z), ("delta_bias", delta_bias), ("state_in", state_in)):
+    of = {"u": u, "delta": delta, "A": A, "B": B, "C": C, "skip": skip, "z": z,
+          "delta_bias": delta_bias, "state_in": state_in}
+    if not g.keys() <= of.keys():
+        raise ValueError(f"outputs go by the inputs' names, got {sorted(g.keys() - of.keys())}")
+    for name, t in of.items():
         if t is None:
             if g.get(name) is not None:
                 raise ValueError(f"outputs[{name!r}]: there is no such input")

@@ -163,3 +163,12 @@ def test_tensors_on_another_device():
         got = block.lbi_rms_norm(x.to("cuda:1"), torch.ones(8, device="cuda:1"))[0]
         assert torch.cuda.current_device() == 0
     assert got.device.index == 1 and torch.equal(got.cpu(), want)
+
+
+@gpu
+def test_outputs_by_a_name_that_no_input_has_are_refused():
+    x, A, B = torch.zeros(6, 8, device=DEV), -torch.ones(8, 2, device=DEV), torch.zeros(6, 2, device=DEV)
+    for name in ("du", "dout", "state_out"):
+        with pytest.raises(ValueError):
+            block.lbi_ssm_scan_backward(x, x, A, B, B, x, outputs={name: torch.empty_like(x)})
+    torch.cuda.synchronize()
