@@ -296,10 +296,6 @@ struct Segment {
         if (end <= t) end = q.T;
     }
 };
-inline Sequences sequences(const int64_t *offsets, int64_t T, int64_t B)
-{
-    return {offsets, T, B, B > 0 ? T / B : 0};
-}
 
 // The row of a state tensor that sequence i uses, or -1.
 __device__ __forceinline__ int64_t state_row(const int32_t *slots, int32_t n_slots, int64_t i)

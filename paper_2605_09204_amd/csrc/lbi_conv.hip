@@ -75,8 +75,7 @@ __device__ __forceinline__ void load_row(const T *p, int left, Raw<T, V> &r)
     if constexpr (FULL) {
         r.load(p, V);
     } else {
-        // a loop that stays one: this is the last lane of a row whose width is no
-        // multiple of V
+        // a row narrower than a vector: the values that are not there repeat the first
         T v[V];
 #pragma unroll
         for (int i = 0; i < V; ++i)

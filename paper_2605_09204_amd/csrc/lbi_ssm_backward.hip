@@ -245,7 +245,7 @@ template <typename T, int NS, bool JOINED>
 __global__ __launch_bounds__(256, waves_of<T>(NS)) void gradient_kernel(const SsmArgs a)
 {
     constexpr int STEP = step_of(NS), NP = 4 * NS;
-    constexpr int V = STEP <= 8 ? 2 : 4;             // channels a thread stages
+    constexpr int V = 2;                             // channels a thread stages
     constexpr int E = (STEP * NP + 255) / 256;       // B (and C) values a thread stages
     constexpr int BROWS = 256 / NP;                  // rows of them staged at once
     constexpr int PER = NS <= 2 ? 4 : (NS == 4 ? 2 : 1);  // tokens whose dB, dC are summed at once
