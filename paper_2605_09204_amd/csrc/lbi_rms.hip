@@ -181,8 +181,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_kernel(const No
 //
 // Rows below 128 features: sum l of L = min(64, the largest power of two up to D) is
 // x_l + x_{l+L}.  Wider ones: the row's vectors of four, which begin where t D + d is a
-// multiple of four; 64 lanes take one each in turn, a lane's four sums grow along the row
-// and are then added in order.  What lies ahead of the first vector or after the last joins
+// multiple of four; 64 lanes (32 below 256 features) take one each in turn, a lane's four sums
+// grow along the row and are then added in order.  What lies ahead of the first vector or after the last joins
 // the first sum of lanes (t D mod 4) .. 3 and 0 .. 2.  The lanes' sums are added pairwise.
 //
 // The squares are exchanged in LDS: element d lies at d + shift, shift = t D mod 4, which
@@ -213,13 +213,15 @@ template <int WIDTH> __device__ __forceinline__ float sum_in_order(const float *
         return lanes_sum<64>(lane < L ? sq[lane] + more : 0.f);
     }
     const RowOrder o(row, D);
+    const int L = D < 256 ? 32 : 64;
     f4 a = {0.f, 0.f, 0.f, 0.f};
     if (lane >= o.shift && lane < o.first)
         a.x = sq[lane];
 #pragma unroll
-    for (int v = lane, k = 0; k < (WIDTH + 255) / 256; v += 64, ++k) {
-        const f4 q = *(const f4 *)(sq + (v < o.vectors ? o.first + 4 * v : 0));
-        if (v < o.vectors)
+    for (int v = lane, k = 0; k < (WIDTH + 255) / 256; v += L, ++k) {
+        const bool there = lane < L && v < o.vectors;
+        const f4 q = *(const f4 *)(sq + (there ? o.first + 4 * v : 0));
+        if (there)
             a += q;
     }
     if (lane < o.tail)

@@ -49,7 +49,8 @@ def formula(x, w, r, fmt, group):
 
 SHAPES = [(4099, 2048), (3001, 768), (777, 4096), (5003, 128), (700, 1111), (2003, 130), (64, 8000),
           (9, 16), (40, 17), (33, 63), (301, 64), (200, 100), (64, 127), (51, 129), (45, 131),
-          (31, 1024), (30, 1025), (23, 2047), (20, 4100), (12, 8127)]
+          (31, 1024), (30, 1025), (23, 2047), (20, 4100), (12, 8127), (6747, 176), (301, 132),
+          (700, 143), (90, 200), (512, 255), (100, 256), (64, 257), (9, 252)]
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
