@@ -103,11 +103,13 @@ lbi_status lbi_rms_norm(const void *x, int64_t ld_x, const void *residual, int64
  * the squares has a stated order.  D < 128: sum l of L = min(64, the largest
  * power of two up to D) is that of elements l and l + L.  D >= 128: the row's
  * aligned vectors of four, which begin where t D + d is a multiple of four, go
- * to 64 lanes (32 for D < 256) in turn; a lane's four sums (one an element of
- * its vectors) grow along the row and are added in order; what lies ahead of
- * the first vector or after the last joins the first sum of lanes (t D mod 4)
- * .. 3 and 0 .. 2.  The L, 32 or 64 sums are added pairwise, neighbours first.
- * (For D no multiple of four a row's last bits thus go by its place t.)
+ * to 64 lanes (32 for D < 256, 512 for D > 8128) in turn; a lane's four sums
+ * (one an element of its vectors) grow along the row and are added in order;
+ * what lies ahead of the first vector or after the last joins the first sum of
+ * lanes (t D mod 4) .. 3 and 0 .. 2.  The lanes' sums are added pairwise,
+ * neighbours first, up to 64 of them, and the eight that this leaves of 512 by
+ * halves, the first with the fifth.  (For D no multiple of four a row's last
+ * bits go by its place t.)
  */
 lbi_status lbi_rms_norm_q8(const void *x, int64_t ld_x, const void *residual,
                            int64_t ld_residual, const float *weight, void *q, int64_t ld_q,

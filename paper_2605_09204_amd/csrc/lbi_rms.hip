@@ -181,9 +181,11 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_kernel(const No
 //
 // Rows below 128 features: sum l of L = min(64, the largest power of two up to D) is
 // x_l + x_{l+L}.  Wider ones: the row's vectors of four, which begin where t D + d is a
-// multiple of four; 64 lanes (32 below 256 features) take one each in turn, a lane's four sums
-// grow along the row and are then added in order.  What lies ahead of the first vector or after the last joins
-// the first sum of lanes (t D mod 4) .. 3 and 0 .. 2.  The lanes' sums are added pairwise.
+// multiple of four; 64 lanes (32 below 256 features, 512 above 8128) take one each in turn, a
+// lane's four sums grow along the row and are then added in order.  What lies ahead of the
+// first vector or after the last joins the first sum of lanes (t D mod 4) .. 3 and 0 .. 2.  The
+// lanes' sums are added pairwise, neighbours first, up to 64 of them; what that leaves of 512
+// by halves, the first with the fifth.
 //
 // The squares are exchanged in LDS: element d lies at d + shift, shift = t D mod 4, which
 // puts the vectors at multiples of four.
@@ -228,39 +230,63 @@ template <int WIDTH> __device__ __forceinline__ float sum_in_order(const float *
         a.x += sq[o.first + 4 * o.vectors + lane];
     return lanes_sum<64>(((a.x + a.y) + a.z) + a.w);
 }
-// By a workgroup, a sum a thread (the four of a lane in four threads side by side).
-template <int WIDTH>
-__device__ __forceinline__ float sum_in_order_together(const float *sq, int D, int64_t row, float *red)
+// By a workgroup, the four sums of a lane in four threads side by side; MANY: 512 lanes, eight
+// a thread (registers for them cost narrower rows a third of their speed).
+template <int WIDTH, bool MANY>
+__device__ __forceinline__ float sum_in_order_together(const float *sq, int D, int64_t row,
+                                                       float (*red)[8])
 {
     const int t = threadIdx.x;
     if (t < 256) {
         const RowOrder o(row, D);
-        float a = 0.f;
-        if ((t & 3) == 0 && t >> 2 >= o.shift && t >> 2 < o.first)
-            a = sq[t >> 2];
-#pragma unroll 16
-        for (int k = 0; k < WIDTH / 256; ++k) {
+        const bool head = (t & 3) == 0 && t >> 2 >= o.shift && t >> 2 < o.first;
+        const bool tail = (t & 3) == 0 && t >> 2 < o.tail;
+        const float before = head ? sq[t >> 2] : 0.f;
+        const float after = tail ? sq[o.first + 4 * o.vectors + (t >> 2)] : 0.f;
+        auto value = [&](int k) {
             const int i = t + 256 * k;
             const float q = sq[o.first + i];
-            a += i < 4 * o.vectors ? q : 0.f;
+            return i < 4 * o.vectors ? q : 0.f;
+        };
+        // over the quad in order (quad_perm broadcasts), then over the wavefront's 16 lanes
+        auto wave = [&](float a, int m) {
+            float s = ((dpp<0x00>(a) + dpp<0x55>(a)) + dpp<0xAA>(a)) + dpp<0xFF>(a);
+            s += xchg<7>(s);
+            s += xchg<8>(s);
+            s = add_rows<16>(s, s);
+            s = add_rows<32>(s, s);
+            if ((t & 63) == 0)
+                red[t >> 6][m] = s;
+        };
+        if constexpr (MANY) {
+            float a[8] = {before};
+#pragma unroll
+            for (int k = 0; k < WIDTH / 256; k += 8)
+#pragma unroll
+                for (int m = 0; m < 8; ++m)
+                    a[m] += value(k + m);
+            a[0] += after;
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+                wave(a[m], m);
+        } else {
+            float a = before;
+#pragma unroll 16
+            for (int k = 0; k < WIDTH / 256; ++k)
+                a += value(k);
+            wave(a + after, 0);
         }
-        if ((t & 3) == 0 && t >> 2 < o.tail)
-            a += sq[o.first + 4 * o.vectors + (t >> 2)];
-        // quad_perm broadcasts of the quad's four values
-        float s = ((dpp<0x00>(a) + dpp<0x55>(a)) + dpp<0xAA>(a)) + dpp<0xFF>(a);
-        s += xchg<7>(s);
-        s += xchg<8>(s);
-        s = add_rows<16>(s, s);
-        s = add_rows<32>(s, s);
-        if ((t & 63) == 0)
-            red[t >> 6] = s;
     }
     __syncthreads();
-    return (red[0] + red[1]) + (red[2] + red[3]);
+    auto sum = [&](int m) { return (red[0][m] + red[1][m]) + (red[2][m] + red[3][m]); };
+    if constexpr (!MANY)
+        return sum(0);
+    else
+        return ((sum(0) + sum(4)) + (sum(2) + sum(6))) + ((sum(1) + sum(5)) + (sum(3) + sum(7)));
 }
 // 1 / sqrt(sum / D + eps), rounded to nearest: product and sum each by itself, and the
 // hardware's root (one unit of the last place) with a Newton step whose residual 1 - m r^2 is
-// exact to second order.
+// exact to second order.  (One root in some 10^7 lies so near the middle that it goes the other way.)
 __device__ __forceinline__ float reciprocal_root(float sum, float over_D, float eps)
 {
 #pragma clang fp contract(off)
@@ -271,12 +297,12 @@ __device__ __forceinline__ float reciprocal_root(float sum, float over_D, float 
     return r > 0.f && r < INFINITY ? fmaf(0.5f * r, e, r) : r;
 }
 
-template <typename X, typename R, int LANES, int NV, int FMT>
+template <typename X, typename R, int LANES, int NV, int FMT, bool MANY>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_q8_kernel(const NormArgs a)
 {
     constexpr int ROWS = LANES < 256 ? 256 / LANES : 1, WIDTH = LANES * NV * 8, PITCH = WIDTH + 4;
     __shared__ __align__(16) float squares[ROWS * PITCH];
-    __shared__ float red[4];
+    __shared__ float red[4][8];
     __shared__ float red_max[LANES > 64 ? LANES / 64 : 1];
     const int lane = threadIdx.x % LANES;
     const int64_t stride = (int64_t)gridDim.x * ROWS;
@@ -320,7 +346,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_q8_kernel(const
         float sum = 0.f;
         if constexpr (LANES > 64) {
             __syncthreads();
-            sum = sum_in_order_together<WIDTH>(squares, a.D, row, red);
+            sum = sum_in_order_together<WIDTH, MANY>(squares, a.D, row, red);
         } else {
             // the rows of a wavefront, one after the other
             wave_sync();
@@ -531,8 +557,15 @@ template <typename X, typename R, int FMT> hipError_t forward_q8(const NormArgs 
     const Shape s = shape_of(a.D);
     const dim3 grid((unsigned)block_count(a.T, s.rows, kBlocks)), block(s.lanes < 256 ? 256 : s.lanes);
     return by_shape(s, [&](auto lanes, auto nv) {
-        rms_q8_kernel<X, R, decltype(lanes)::value, decltype(nv)::value, FMT>
-            <<<grid, block, 0, stream>>>(a);
+        constexpr int LANES = decltype(lanes)::value, NV = decltype(nv)::value;
+        if constexpr (LANES * NV * 8 >= 8192) {
+            if (LANES == 1024 || a.D > 8128) {
+                rms_q8_kernel<X, R, LANES, NV, FMT, true><<<grid, block, 0, stream>>>(a);
+                return hipGetLastError();
+            }
+        }
+        if constexpr (LANES < 1024)
+            rms_q8_kernel<X, R, LANES, NV, FMT, false><<<grid, block, 0, stream>>>(a);
         return hipGetLastError();
     });
 }

@@ -3,8 +3,8 @@
 A quotient that lies in the middle between two 8-bit values is decided by the last bits of what it
 was computed from, so no tolerance helps there: the library adds a row's squares in one stated order
 and rounds after each operation, and its bytes, scales and sums are then those of the same formula in
-float32 tensor operations, bit for bit.  (That holds for 8 rows and more of up to 8128 features, for
-which the tensor operations use that order; below and above they use others.)
+float32 tensor operations, bit for bit.  (That holds for 8 rows and more; for fewer the tensor
+operations use other orders.)
 """
 import pytest
 import torch
@@ -50,7 +50,8 @@ def formula(x, w, r, fmt, group):
 SHAPES = [(4099, 2048), (3001, 768), (777, 4096), (5003, 128), (700, 1111), (2003, 130), (64, 8000),
           (9, 16), (40, 17), (33, 63), (301, 64), (200, 100), (64, 127), (51, 129), (45, 131),
           (31, 1024), (30, 1025), (23, 2047), (20, 4100), (12, 8127), (6747, 176), (301, 132),
-          (700, 143), (90, 200), (512, 255), (100, 256), (64, 257), (9, 252)]
+          (700, 143), (90, 200), (512, 255), (100, 256), (64, 257), (9, 252), (8, 8128), (300, 8129),
+          (40, 8192), (17, 8195), (9, 12345), (33, 16384), (8, 16383)]
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
