@@ -77,7 +77,8 @@ typedef enum {
  *   T >= 0, 1 <= D <= LBI_NORM_MAX_D, eps >= 0 (else LBI_ERR_SHAPE).
  * residual_out may be the same pointer as residual (with the same stride).
  * A row of zeros gives zeros (eps > 0); a NaN or an infinity gives NaN in its
- * row.
+ * row.  The sum of the squares is float32: where it passes that range (values
+ * of 10^19 / sqrt(D) and more) finite values give zeros.
  */
 lbi_status lbi_rms_norm(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual,
                         const float *weight, void *out, int64_t ld_out, void *residual_out,

@@ -203,7 +203,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 def _stream(dev: int) -> int:
     """The current stream of the device, as the library takes it."""
-    return _raw_stream(dev) if _raw_stream is not None else _stream_ptr(None, torch.device("cuda", dev))
+    if _raw_stream is not None:
+        return _raw_stream(dev)
+    return _stream_ptr(None, torch.device("cuda", dev))
 
 
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device

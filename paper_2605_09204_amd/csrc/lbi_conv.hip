@@ -11,7 +11,7 @@
 //
 // Measured, four taps, bf16, 1536 channels: 8201 packed tokens of 13 sequences, 51 MB, in
 // 14.5 us (3.5 TB/s; a copy of as many bytes 8.4 us); the gradient of 16384 tokens, 151 MB,
-// in 34 + 4 us (4.0 TB/s); one token of 64 sequences 5.6 us, of which a launch is most.
+// in 35 + 4 us (3.9 TB/s); one token of 64 sequences 5.3 us, dependent trips to memory.
 #include "lbi_block.hpp"
 
 namespace lbi {

@@ -16,7 +16,7 @@
 //
 // Measured, bf16 with the residual: 16384 rows of 768 features, 101 MB: forward
 // 16 us (6.3 TB/s; a copy of as many bytes 15.7 us), gradient 20 + 4 us (4.1 TB/s);
-// 4099 rows of 2048 to E4M3 by groups of 128, 59 MB: 13.4 us (4.4 TB/s; 12.2 with the squares
+// 4099 rows of 2048 to E4M3 by groups of 128, 59 MB: 14.5 us (4.1 TB/s; one less with the squares
 // added in registers, in no stated order).
 #include "lbi_block.hpp"
 
@@ -206,7 +206,8 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_wave_barrier();
 }
 // By a wavefront; WIDTH: most features.
-template <int WIDTH> __device__ __forceinline__ float sum_in_order(const float *sq, int D, int64_t row)
+template <int WIDTH>
+__device__ __forceinline__ float sum_in_order(const float *sq, int D, int64_t row)
 {
     const int lane = threadIdx.x & 63;
     if (D < 128) {
@@ -286,7 +287,8 @@ __device__ __forceinline__ float sum_in_order_together(const float *sq, int D, i
 }
 // 1 / sqrt(sum / D + eps), rounded to nearest: product and sum each by itself, and the
 // hardware's root (one unit of the last place) with a Newton step whose residual 1 - m r^2 is
-// exact to second order.  (One root in some 10^7 lies so near the middle that it goes the other way.)
+// exact to second order.  (One root in some 10^7 lies so near the middle that it goes the other
+// way.)
 __device__ __forceinline__ float reciprocal_root(float sum, float over_D, float eps)
 {
 #pragma clang fp contract(off)
@@ -354,7 +356,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rms_q8_kernel(const
             const int first = (threadIdx.x >> 6) * PER_WAVE;
 #pragma unroll
             for (int k = 0; k < PER_WAVE; ++k) {
-                const float v = sum_in_order<WIDTH>(squares + (first + k) * PITCH, a.D, base + first + k);
+                const float v =
+                    sum_in_order<WIDTH>(squares + (first + k) * PITCH, a.D, base + first + k);
                 if (PER_WAVE == 1 || (int)(threadIdx.x & 63) / LANES == k)
                     sum = v;
             }
@@ -504,7 +507,9 @@ struct Shape {
 };
 // Up to 1024 features a wavefront takes a row, above that a workgroup: measured in bf16
 // at 64 to 16384 rows, a workgroup instead costs rows of 1024 features 3 to 26 per cent forward
-// and up to 61 in the gradient, and a wavefront instead costs rows of 2048 up to 24 forward.
+// and up to 61 in the gradient, and a wavefront instead costs rows of 2048 up to 24 forward.  From
+// 4097 to 8192 features 1024 lanes instead of 256 change the forward by 0 to 5 per cent either
+// way and the gradient (bf16) from 39.6 to 33.7 us at 3000 rows of 4100, from 21.3 to 23.7 at 1500 of 8192.
 Shape shape_of(int32_t D)
 {
     const int vec = (D + 7) / 8;

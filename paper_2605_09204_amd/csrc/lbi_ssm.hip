@@ -14,10 +14,10 @@
 // their sequence.  Sequences begin and end anywhere in a range.
 //
 // Measured, 16 states, bf16, gated: 16384 tokens of 1536 channels in 8 sequences
-// 200 us (first walk 84, carry 5, second walk 111; the vector ALUs issue in 85 to 95 % of
+// 202 us (first walk 84, carry 6, second walk 113; the vector ALUs issue in 90 and 95 % of
 // the cycles that a CU is busy; walking such sequences once, 192 workgroups, takes
 // longer than twice in ranges that fill the GPU); 32768 tokens of one sequence of 768
-// channels in float32 217 us (91, 7, 119); one token of 64 sequences, 13.5 MB, 5.6 us.
+// channels in float32 214 us (88, 10, 116); one token of 64 sequences, 13.5 MB, 5.7 us.
 #include "lbi_ssm.hpp"
 
 namespace lbi {

@@ -209,8 +209,9 @@ __device__ __forceinline__ float sum_states(const float (&v)[4])
 // memory, so each of WAVES wavefronts has the ends of DEEP consecutive ranges in flight;
 // the wavefronts exchange what their ranges do to a state that enters them (the end from zero, and
 // the power of two that decays it), and each then walks its ranges again from the state that does enter.
-// The ranges of 32768 tokens, 12288 states: 7.4 us, one wavefront in batches of 32 ranges 15.4.
-// Up to 8 ranges one trip does, with one wavefront (5.5 us for 8 sequences of 24576 states).
+// The ranges of 32768 tokens, 12288 states: 9.6 us (with decays as plain factors, which overflow
+// where a channel grows, 7.4; so by one wavefront in batches of 32 ranges 15.4).
+// Up to 8 ranges one trip does, with one wavefront (5.6 us for 8 sequences of 24576 states).
 template <int DEEP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void carry_kernel(const SsmArgs a)
 {

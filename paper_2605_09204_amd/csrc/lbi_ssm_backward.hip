@@ -25,8 +25,8 @@
 // the sums over tokens (dA, dskip, ddelta_bias), range by range.
 //
 // Measured, 16 states, bf16, gated, 16384 tokens of 1536 channels in 8 sequences:
-// 540 us (first walk 150, carry 8, second walk 368, sums of dB and dC 10, of the
-// parameters 5; the vector ALUs issue in 92 % of the first walk's and 83 % of the second's
+// 555 us (first walk 152, carry 8, second walk 380, sums of dB and dC 10, of the
+// parameters 5; the vector ALUs issue in 93 % of the first walk's and 83 % of the second's
 // busy cycles, and the second's last workgroups leave a sixth of the CUs idle at its end).
 #include "lbi_ssm.hpp"
 
