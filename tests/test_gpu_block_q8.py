@@ -3,8 +3,8 @@
 A quotient that lies in the middle between two 8-bit values is decided by the last bits of what it
 was computed from, so no tolerance helps there: the library adds a row's squares in one stated order
 and rounds after each operation, and its bytes, scales and sums are then those of the same formula in
-float32 tensor operations, bit for bit.  (That holds for 8 rows and more; for fewer the tensor
-operations use other orders.)
+float32 tensor operations, bit for bit.  (That holds for 8 rows and more and up to 2^24 values; for
+fewer rows the tensor operations use other orders, for more values another 1 / D.)
 """
 import pytest
 import torch
