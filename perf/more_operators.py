@@ -220,36 +220,36 @@ def prepare(case, seed):
 # ---- the library's operators -------------------------------------------------
 
 def _run_own(s):
-    from paper_2605_09204_amd import block
+    from paper_2605_09204_amd import linear
 
     c = s["case"]
     op = c["op"]
     get = s.get
     if op == "norm":
-        return block.lbi_layer_norm(s["x"], get("weight"), get("bias"), get("residual"), EPS)
+        return linear.lbi_layer_norm(s["x"], get("weight"), get("bias"), get("residual"), EPS)
     if op == "norm_backward":
-        return block.lbi_layer_norm_backward(s["dout"], s["x"], get("weight"), get("dresidual"),
-                                             EPS)
+        return linear.lbi_layer_norm_backward(s["dout"], s["x"], get("weight"), get("dresidual"),
+                                              EPS)
     if op.startswith("projection"):
-        act = {"none": block.LBI_ACT_NONE, "silu": block.LBI_ACT_SILU,
-               "gelu": block.LBI_ACT_GELU}[c["act"]]
+        act = {"none": linear.LBI_ACT_NONE, "silu": linear.LBI_ACT_SILU,
+               "gelu": linear.LBI_ACT_GELU}[c["act"]]
         if op == "projection_backward":
-            return block.lbi_projection_backward(s["x"], s["weight"], s["dout"], act, get("pre"))
+            return linear.lbi_projection_backward(s["x"], s["weight"], s["dout"], act, get("pre"))
         out = torch.empty(c["T"], c["N"], dtype=STORE[c["stream"]], device="cuda")
         pre = torch.empty(c["T"], c["N"], dtype=s["x"].dtype, device="cuda") if c["pre"] else None
-        block.lbi_projection(s["x"], s["weight"], get("bias"), act, get("residual"), out=out,
-                             pre=pre)
+        linear.lbi_projection(s["x"], s["weight"], get("bias"), act, get("residual"), out=out,
+                              pre=pre)
         return out, pre
     a = (s["q"], s["k"], s["v"], s["log_decay"])
     if op == "attention_step":
         new = torch.empty_like(s["state_in"])
-        return block.lbi_linear_attention_step(*a, s["state_in"], new, s["scale"]), new
+        return linear.lbi_linear_attention_step(*a, s["state_in"], new, s["scale"]), new
     kw = {"scale": s["scale"], "offsets": get("offsets"), "sequences": c["B"],
           "state_in": get("state_in")}
     if op == "attention":
         new = torch.empty_like(s["state_in"]) if c["states"] else None
-        return block.lbi_linear_attention(*a, state_out=new, **kw), new
-    return block.lbi_linear_attention_backward(*a, s["dout"], dstate_out=get("dstate_out"), **kw)
+        return linear.lbi_linear_attention(*a, state_out=new, **kw), new
+    return linear.lbi_linear_attention_backward(*a, s["dout"], dstate_out=get("dstate_out"), **kw)
 
 
 # ---- their plain forms, in float32 -------------------------------------------
