@@ -21,12 +21,15 @@ CSRC = os.path.join(PKG, "csrc")
 SOURCES = ["lbi_chain_f32.hip", "lbi_chain_f32x.hip", "lbi_chain_bf16.hip", "lbi_chain_bf16r1.hip",
            "lbi_chain_wave.hip", "lbi_chain_wide.hip",
            "lbi_chain_ksplit.hip", "lbi_tree.hip", "lbi_chain_ring.hip", "lbi_aux.hip", "lbi_norms.hip", "lbi_region.hip",
-           "lbi_rms.hip", "lbi_conv.hip", "lbi_ssm.hip", "lbi_ssm_backward.hip", "lbi_block_api.hip", "lbi_api.hip"]
+           "lbi_rms.hip", "lbi_layer_norm.hip", "lbi_conv.hip", "lbi_ssm.hip", "lbi_ssm_backward.hip",
+           "lbi_attention.hip", "lbi_attention_backward.hip", "lbi_projection.hip",
+           "lbi_block_api.hip", "lbi_linear_api.hip", "lbi_api.hip"]
 # Sources none of whose kernels may use scratch memory, for vector registers or for scalar ones.  A
 # build of the gradient kernel that spilled vector registers gave wrong values wherever lanes load
 # partial rows, and the same code with more registers did not; why has not been shown.  The build
 # fails if a kernel spills, so that what is tested is what runs.
-NO_SPILLS = {"lbi_rms.hip", "lbi_conv.hip", "lbi_ssm.hip", "lbi_ssm_backward.hip"}
+NO_SPILLS = {"lbi_rms.hip", "lbi_layer_norm.hip", "lbi_conv.hip", "lbi_ssm.hip", "lbi_ssm_backward.hip",
+             "lbi_attention.hip", "lbi_attention_backward.hip", "lbi_projection.hip"}
 _USAGE = "kernel-resource-usage"
 INCLUDE = os.path.join(ROOT, "include")
 LIBDIR = os.path.join(PKG, "_lib")

@@ -20,11 +20,13 @@ struct NormArgs {
     const void *x;          // [T][D] token type (gradient: dout)
     const void *residual;   // [T][D] residual type, or NULL (gradient: dresidual)
     const void *s;          // gradient: [T][D] residual type, what was normalised
-    const float *weight;    // [D]
+    const float *weight;    // [D] (layer norm: or NULL)
+    const float *bias;      // layer norm: [D] or NULL
     void *out;              // [T][D] token type; bytes for 8-bit forms; gradient: ds
     void *residual_out;     // [T][D] residual type, or NULL
     float *scales;          // 8-bit forms: [T][ngroups]
-    float *partial;         // gradient: [blocks][D] partial sums of dweight, or NULL
+    float *partial;         // gradient: [blocks][D] partial sums of dweight (layer norm:
+                            // [blocks][2][D], dbias behind it), or NULL
     int64_t ld_x, ld_residual, ld_s, ld_out, ld_residual_out;
     int64_t T;
     int32_t D;

@@ -1,0 +1,371 @@
+// Matrix products with bias, activation and residual in their epilogue, and what the gradient of
+// one needs beside two more products.
+//
+//   out = act(x W^T + bias) + residual;   dz = dout act'(z), dx = dz W, dW = dz^T x
+//
+// The three differ in how the operands lie: the index that is summed runs along the rows of both
+// (forward), of one (dx) or of none (dW).  A workgroup takes a BM x BN tile of the result, the
+// operands pass through LDS as they lie, and the matrix instructions' operands are read from there
+// straight or through the transposing read.
+#include "lbi_attention.hpp"
+
+namespace lbi {
+namespace {
+
+// ---- activations
+
+template <int ACT> __device__ __forceinline__ float activate(float z)
+{
+    if constexpr (ACT == LBI_ACT_SILU)
+        return silu(z);
+    else if constexpr (ACT == LBI_ACT_GELU)
+        return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    else
+        return z;
+}
+template <int ACT> __device__ __forceinline__ float slope(float z)
+{
+    if constexpr (ACT == LBI_ACT_SILU)
+        return silu_slope(z, sigmoid(z));
+    else if constexpr (ACT == LBI_ACT_GELU)  // z times the normal density vanishes at the ends
+        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) +
+               z * __builtin_amdgcn_exp2f(fmaxf(-0.5f * kLog2e * z * z, -200.f)) * 0.39894228040143268f;
+    else
+        return 1.f;
+}
+
+// ---- the product
+
+// Operand of 32 values k from a tile in LDS: bf16 in their order, 8 g .. 8 g + 7 in lane group g.
+template <typename T, bool COLS>
+__device__ __forceinline__ void operand(Frag<T> &f, const T *m, int stride, int row0, int k0)
+{
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (COLS) f.cols(m, stride, k0, row0);
+        else f.rows(m, stride, row0, k0);
+    } else if constexpr (COLS) {
+        const int lane = threadIdx.x & 63, c = lane & 15;
+        const T *p = m + (k0 + 8 * (lane >> 4) + (c >> 2)) * stride + row0 + 4 * (c & 3);
+        typedef __attribute__((address_space(3))) s4 lds_s4;
+        const u2 a = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)p));
+        const u2 b = __builtin_bit_cast(
+            u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(p + 4 * stride)));
+        f.w = u4{a.x, a.y, b.x, b.y};
+    } else {
+        const int lane = threadIdx.x & 63;
+        f.w = *(const u4 *)(m + (row0 + (lane & 15)) * stride + k0 + 8 * (lane >> 4));
+    }
+}
+
+// A tile of an operand: [SIZE][BK] of rows or [BK][SIZE], in registers on its way to LDS.
+template <typename T, bool COLS, int SIZE, int BK> struct Staged {
+    static constexpr int WIDTH = COLS ? SIZE : BK, HEIGHT = COLS ? BK : SIZE;
+    static constexpr int STRIDE = WIDTH + (COLS ? 32 : 16) / (int)sizeof(T);
+    static constexpr int PER_ROW = WIDTH / 8, COUNT = WIDTH * HEIGHT / 8 / 256;
+    Raw<T, 8> r[COUNT];
+
+    // rows: how many of them are there from first on; k: likewise
+    __device__ __forceinline__ void load(const T *p, int64_t ld, int64_t first, int64_t rows,
+                                         int64_t k0, int64_t k)
+    {
+        const int64_t down = COLS ? k : rows, across = COLS ? rows : k;
+        const T *base = p + (COLS ? k0 * ld + first : first * ld + k0);
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const int at = i * 256 + threadIdx.x, y = at / PER_ROW, x = at % PER_ROW * 8;
+            const int64_t left = y < down ? across - x : 0;
+            r[i].load(base + (left > 0 ? y * ld + x : 0), left > 8 ? 8 : (int)left);
+        }
+    }
+    __device__ __forceinline__ void put(T *m) const
+    {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const int at = i * 256 + threadIdx.x, y = at / PER_ROW, x = at % PER_ROW * 8;
+            T *to = m + y * STRIDE + x;
+            if constexpr (sizeof(T) == 2) {
+                *(u4 *)to = u4{r[i].w[0], r[i].w[1], r[i].w[2], r[i].w[3]};
+            } else {
+                *(f4 *)to = f4{r[i].v[0], r[i].v[1], r[i].v[2], r[i].v[3]};
+                *(f4 *)(to + 4) = f4{r[i].v[4], r[i].v[5], r[i].v[6], r[i].v[7]};
+            }
+        }
+    }
+};
+
+// Four sums of a row of the result, n .. n + 3, through the epilogue.
+template <typename T, typename O, int ACT>
+__device__ __forceinline__ void finish_as(const ProductArgs &a, int64_t m, int n, f4 v)
+{
+    const int left = a.N - n;
+    if (a.bias) {
+        float b[4];
+        load_some<4>(a.bias + n, left, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] += b[i];
+    }
+    if (a.pre)
+        store4((T *)a.pre + m * a.ld_pre + n, left, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        v[i] = activate<ACT>(v[i]);
+    if (a.residual) {
+        float r[4];
+        load_some<4>((const O *)a.residual + m * a.ld_residual + n, left, r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] += r[i];
+    }
+    store4((O *)a.out + m * a.ld_out + n, left, v);
+}
+template <typename T, int ACT>
+__device__ __forceinline__ void finish(const ProductArgs &a, int64_t m, int n, const f4 &v)
+{
+    if (a.out_bf16) finish_as<T, bf16_bits, ACT>(a, m, n, v);
+    else finish_as<T, float, ACT>(a, m, n, v);
+}
+
+template <typename T, bool A_COLS, bool B_COLS, int BM, int BN, int ACT>
+__global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs a, int64_t first)
+{
+    constexpr int BK = 128 / (int)sizeof(T);
+    using Sa = Staged<T, A_COLS, BM, BK>;
+    using Sb = Staged<T, B_COLS, BN, BK>;
+    __shared__ __align__(16) T tile_a[2][Sa::HEIGHT * Sa::STRIDE], tile_b[2][Sb::HEIGHT * Sb::STRIDE];
+    constexpr int MT = BM / 32, NT = BN / 32;  // 16 x 16 results of a wavefront, a quarter of the tile
+    const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
+    const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
+    const int across = (a.N + BN - 1) / BN;
+    uint32_t id = blockIdx.x;
+    // Workgroups go to the eight XCDs in turn; each gets tiles that lie together, whose operands
+    // its L2 then holds for all of them.
+    if (gridDim.x % 8 == 0)
+        id = id % 8 * (gridDim.x / 8) + id / 8;
+    const int n0 = (int)(id % across) * BN;
+    const int64_t rest = first + id / across;
+    const int64_t m0 = rest / a.splits * BM;
+    const int64_t k_first = rest % a.splits * a.split;
+    const int64_t k_end = k_first + a.split < a.K ? k_first + a.split : a.K;
+    f4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    Sa sa;
+    Sb sb;
+    auto load = [&](int64_t k) {
+        sa.load((const T *)a.a, a.ld_a, m0, a.M - m0, k, k_end - k);
+        sb.load((const T *)a.b, a.ld_b, n0, a.N - n0, k, k_end - k);
+    };
+    load(k_first);
+    int at = 0;
+    for (int64_t k = k_first; k < k_end; k += BK) {
+        sa.put(tile_a[at]);
+        sb.put(tile_b[at]);
+        __syncthreads();
+        if (k + BK < k_end)
+            load(k + BK);
+#pragma unroll
+        for (int kb = 0; kb < BK; kb += 32) {
+            Frag<T> fb[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                operand<T, B_COLS>(fb[j], tile_b[at], Sb::STRIDE, wn + 16 * j, kb);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                Frag<T> fa;
+                operand<T, A_COLS>(fa, tile_a[at], Sa::STRIDE, wm + 16 * i, kb);
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+                    mma(acc[i][j], fb[j], fa);
+            }
+        }
+        at ^= 1;
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int64_t m = m0 + wm + 16 * i + c16;
+            const int n = n0 + wn + 16 * j + 4 * g;
+            if (m >= a.M || n >= a.N)
+                continue;
+            if (a.splits > 1)
+                store4(a.partial + ((rest % a.splits) * a.M + m) * a.N + n, a.N - n, acc[i][j]);
+            else
+                finish<T, ACT>(a, m, n, acc[i][j]);
+        }
+}
+
+// The sum of the splits' partial results, in order, through the epilogue.
+template <typename T, int ACT>
+__global__ __launch_bounds__(256) void join_kernel(const ProductArgs a)
+{
+    const int64_t per = (a.N + 3) / 4, count = a.M * per, size = a.M * a.N;
+    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < count;
+         id += (int64_t)gridDim.x * 256) {
+        const int64_t m = id / per;
+        const int n = (int)(id % per) * 4;
+        const float *p = a.partial + m * a.N + n;
+        f4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < a.splits; ++s) {
+            float x[4];
+            load_some<4>(p + s * size, a.N - n, x);
+            v += f4{x[0], x[1], x[2], x[3]};
+        }
+        finish<T, ACT>(a, m, n, v);
+    }
+}
+
+// ---- dz
+
+constexpr int kSlopeWidth = 512;  // columns of a wavefront, eight a lane
+
+template <typename T, typename O, int ACT>
+__global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a, int row_blocks)
+{
+    __shared__ float sums[4][kSlopeWidth];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = blockIdx.x / row_blocks * kSlopeWidth + lane * 8, left = a.N - n;
+    const int64_t block = blockIdx.x % row_blocks;
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int64_t step = (int64_t)row_blocks * 4;
+#pragma unroll 2
+    for (int64_t t = block * 4 + wave; t < a.T; t += step) {
+        float d[8];
+        load_some<8>((const O *)a.dout + t * a.ld_dout + n, left, d);
+        if constexpr (ACT != LBI_ACT_NONE) {
+            float z[8];
+            load_some<8>((const T *)a.pre + t * a.ld_pre + n, left, z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                d[i] *= slope<ACT>(z[i]);
+        }
+        if (a.dz)
+            store_some<8>((T *)a.dz + t * a.N + n, left, d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            sum[i] += d[i];
+    }
+    if (!a.partial)
+        return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        sums[wave][lane * 8 + i] = sum[i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < kSlopeWidth; c += 256) {
+        const int at = blockIdx.x / row_blocks * kSlopeWidth + c;
+        if (at < a.N)
+            a.partial[block * a.N + at] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
+    }
+}
+
+struct ToVector {
+    float *out;
+    __device__ __forceinline__ void operator()(int64_t c, float v) const { out[c] = v; }
+};
+
+template <typename F> hipError_t by_activation(lbi_activation act, F &&f)
+{
+    if (act == LBI_ACT_SILU) return f(std::integral_constant<int, LBI_ACT_SILU>{});
+    if (act == LBI_ACT_GELU) return f(std::integral_constant<int, LBI_ACT_GELU>{});
+    return f(std::integral_constant<int, LBI_ACT_NONE>{});
+}
+
+// The tile: 128 x 128, or 64 x 64 where those would leave CUs without work.
+int tile_of(const ProductArgs &a)
+{
+    const int64_t big = (a.M + 127) / 128 * ((a.N + 127) / 128);
+    return big >= 256 || a.K >= 4096 ? 128 : 64;
+}
+
+template <typename T, bool A_COLS, bool B_COLS, int TILE, int ACT>
+hipError_t product(const ProductArgs &a, hipStream_t stream)
+{
+    const int64_t across = (a.N + TILE - 1) / TILE, down = (a.M + TILE - 1) / TILE;
+    return in_launches(down * a.splits, across, [&](int64_t first, dim3 grid) {
+        product_kernel<T, A_COLS, B_COLS, TILE, TILE, ACT><<<grid, 256, 0, stream>>>(a, first);
+    });
+}
+template <typename T> hipError_t product_by(const ProductArgs &a, hipStream_t stream)
+{
+    const bool big = tile_of(a) == 128;
+    hipError_t e;
+    if (a.a_cols)
+        e = big ? product<T, true, true, 128, LBI_ACT_NONE>(a, stream)
+                : product<T, true, true, 64, LBI_ACT_NONE>(a, stream);
+    else if (a.b_cols)
+        e = big ? product<T, false, true, 128, LBI_ACT_NONE>(a, stream)
+                : product<T, false, true, 64, LBI_ACT_NONE>(a, stream);
+    else
+        e = by_activation(a.act, [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+            return big ? product<T, false, false, 128, ACT>(a, stream)
+                       : product<T, false, false, 64, ACT>(a, stream);
+        });
+    if (e != hipSuccess || a.splits <= 1)
+        return e;
+    const int64_t n = (a.M * ((a.N + 3) / 4) + 255) / 256;
+    return by_activation(a.act, [&](auto act) {
+        join_kernel<T, decltype(act)::value>
+            <<<dim3((unsigned)(n < 8192 ? n : 8192)), 256, 0, stream>>>(a);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace
+
+int64_t plan_product(ProductArgs &a)
+{
+    const int tile = tile_of(a);
+    const int64_t tiles = (a.M + tile - 1) / tile * ((a.N + tile - 1) / tile);
+    const int64_t unit = a.bf16 ? 64 : 32;
+    const int64_t steps = (a.K + unit - 1) / unit;
+    // two workgroups a CU, and at least eight steps each
+    int64_t splits = 512 / tiles;
+    if (splits > steps / 8) splits = steps / 8;
+    if (splits < 1) splits = 1;
+    const int64_t per = steps > 0 ? (steps + splits - 1) / splits : 1;
+    a.split = per * unit;
+    a.splits = steps > 0 ? (int32_t)((steps + per - 1) / per) : 1;
+    return a.splits > 1 ? a.splits * a.M * a.N : 0;
+}
+
+hipError_t launch_product(const ProductArgs &a, hipStream_t stream)
+{
+    return a.bf16 ? product_by<bf16_bits>(a, stream) : product_by<float>(a, stream);
+}
+
+int64_t slope_rows(int64_t T)
+{
+    const int64_t n = (T + 15) / 16;
+    return n < 512 ? n : 512;
+}
+
+hipError_t launch_slope(const SlopeArgs &a, float *dbias, hipStream_t stream)
+{
+    if (a.T > 0) {
+        const int blocks = (int)slope_rows(a.T);
+        const dim3 grid((unsigned)((a.N + kSlopeWidth - 1) / kSlopeWidth * blocks));
+        hipError_t e = by_activation(a.act, [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+            if (a.bf16) {
+                if (a.out_bf16) slope_kernel<bf16_bits, bf16_bits, ACT><<<grid, 256, 0, stream>>>(a, blocks);
+                else slope_kernel<bf16_bits, float, ACT><<<grid, 256, 0, stream>>>(a, blocks);
+            } else {
+                if (a.out_bf16) slope_kernel<float, bf16_bits, ACT><<<grid, 256, 0, stream>>>(a, blocks);
+                else slope_kernel<float, float, ACT><<<grid, 256, 0, stream>>>(a, blocks);
+            }
+            return hipGetLastError();
+        });
+        if (e != hipSuccess)
+            return e;
+    }
+    if (!dbias)
+        return hipSuccess;
+    return sum_rows(a.partial, a.T > 0 ? slope_rows(a.T) : 0, a.N, a.N, ToVector{dbias}, stream);
+}
+
+}  // namespace lbi
