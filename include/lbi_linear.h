@@ -33,6 +33,7 @@ extern "C" {
 #define LBI_PROJECTION_MAX 65536    /* most features of a projection, in or out     */
 #define LBI_ATTENTION_MAX_DIM 128   /* longest key and longest value of a head      */
 #define LBI_ATTENTION_MAX_H 1024    /* most heads                                   */
+#define LBI_ATTENTION_MAX_LD (1 << 23) /* longest row stride of the tensors it reads  */
 
 /*
  * Layer norm with the residual's addition.

@@ -22,8 +22,14 @@ namespace {
 
 constexpr int C = kAttentionTile;
 
-template <typename T, int DK, int DV>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 || DK + DV == 128) ? 2 : 1) void attention_kernel(const AttentionArgs a, int64_t first)
+// Workgroups of a CU that the registers are divided among, by the widths of a key and a value.
+template <typename T> constexpr int resident(int widths)
+{
+    return widths == 256 ? 1 : widths == 192 ? (sizeof(T) == 2 ? 2 : 1) : (sizeof(T) == 2 ? 3 : 2);
+}
+
+template <typename T, int DK, int DV, bool FULL>
+__global__ __launch_bounds__(256, resident<T>(DK + DV)) void attention_kernel(const AttentionArgs a, int64_t first)
 {
     constexpr int QS = tile_stride<T>(DK), VS = tile_stride<T>(DV), PS = tile_stride<T>(C);
     __shared__ __align__(16) T tile_q[C * QS], tile_k[C * QS], tile_v[C * VS], tile_p[C * PS];
@@ -31,7 +37,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || DK + DV == 128) ? 2 : 1) vo
     const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
     const int h = blockIdx.x % a.in.H, kh = h / (a.in.H / a.in.KH);
     const int64_t range = first + blockIdx.x / a.in.H;
-    const int dk = a.in.DK, dv = a.in.DV;
+    const int dk = FULL ? DK : a.in.DK, dv = FULL ? DV : a.in.DV;
     const int64_t size = (int64_t)dk * dv;
     const float l2 = log2_decay(a.in.log_decay, h), scale = a.in.scale;
     const T *q0 = (const T *)a.in.q + h * dk, *k0 = (const T *)a.in.k + kh * dk;
@@ -40,42 +46,35 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || DK + DV == 128) ? 2 : 1) vo
 
     const Sequences seqs = sequences_of(a.in);
     const Rows rows(a, range);
-    Segment seg;
-    seg.enter(seqs, rows.first, true);
-    State<T, DK, DV> state;
-    auto begin = [&] {
-        const int64_t row = a.in.state_in ? state_row(a.slots, a.n_slots, seg.seq) : -1;
-        const float *p = row >= 0 ? a.in.state_in + (row * a.in.H + h) * size : nullptr;
-        if (a.starts && seg.end > rows.end)  // another workgroup may have written the slot
-            p = a.starts + (range * a.in.H + h) * size;
-        state.load(p, dk, dv, dv, 1);
-    };
-    if (seg.start < rows.first)
-        state.load(a.ends + ((range - 1) * a.in.H + h) * size, dk, dv, dv, 1);
-    else
-        begin();
-    float w[C / 4];
+    State<T, DK, DV, FULL> state;
+    f4 fade[kCausalTiles<C>];
+    causal_fade<C>(fade, l2, scale);
+    float w[C / 4];  // what is left of the tile's tokens at its end
     int weights_of = 0;
-    for (int64_t t = rows.first; t < rows.end;) {
-        const int64_t stop = seg.end < rows.end ? seg.end : rows.end;
-        int n = stop - t < C ? (int)(stop - t) : C;
-        auto load = [&](int n) {
-            bool bad = load_tile<T, C, DK>(tile_q, q0 + t * a.in.ld_q, a.in.ld_q, n, dk);
-            bad |= load_tile<T, C, DK>(tile_k, k0 + t * a.in.ld_k, a.in.ld_k, n, dk);
-            bad |= load_tile<T, C, DV>(tile_v, v0 + t * a.in.ld_v, a.in.ld_v, n, dv);
-            return any_bad(bad, flags);
-        };
-        if (load(n) && n > 1) {
-            n = 1;
-            __syncthreads();
-            load(n);
-        }
-        if (n != weights_of) {
-            to_end<C>(w, l2, n);
-            weights_of = n;
+    // what is left of the state at the tile's first tokens, and 16 tokens on
+    const float reach0 = power(l2, (float)(c16 + 1)) * scale, reach16 = power(l2, 16.f);
+
+    TileLoad<T, C, DK, FULL> next_q, next_k;
+    TileLoad<T, C, DV, FULL> next_v;
+    auto load = [&](int64_t t, int n) {
+        next_q.load(q0 + t * a.in.ld_q, a.in.ld_q, n, dk);
+        next_k.load(k0 + t * a.in.ld_k, a.in.ld_k, n, dk);
+        next_v.load(v0 + t * a.in.ld_v, a.in.ld_v, n, dv);
+    };
+    auto put = [&] {
+        bool bad = next_q.put(tile_q);
+        bad |= next_k.put(tile_k);
+        bad |= next_v.put(tile_v);
+        return any_bad(bad, flags);
+    };
+    // Tokens t .. t + tokens - 1, whose tiles are in LDS, from the state before them.
+    auto work = [&](int64_t t, int tokens) {
+        if (tokens != weights_of) {
+            to_end<C>(w, l2, tokens);
+            weights_of = tokens;
         }
         // p_ij = scale a^(i-j) q_i . k_j, rounded to the tokens' type as an operand
-        causal_tiles<C>([&](int it, int jt) {
+        causal_tiles<C>([&](int at, int it, int jt) {
             f4 p = {0.f, 0.f, 0.f, 0.f};
             if (jt <= it) {
 #pragma unroll
@@ -88,9 +87,9 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || DK + DV == 128) ? 2 : 1) vo
                 const int lag = 16 * (it - jt) + c16 - 4 * g;
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    p[r] = lag >= r ? p[r] * (power(l2, (float)(lag - r)) * scale) : 0.f;
+                    p[r] = lag >= r ? p[r] * fade[at][r] : 0.f;
             }
-            put4(tile_p + (16 * it + c16) * PS + 16 * jt + 4 * g, p);
+            put4(tile_p + (16 * it + c16) * PS + 16 * jt + lane_quad<T>(), p);
         });
         __syncthreads();
 #pragma unroll
@@ -104,7 +103,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || DK + DV == 128) ? 2 : 1) vo
 #pragma unroll
             for (int b = 0; b < DK / 32; ++b)
                 pack_tiles(fs[b], state.s[2 * b][c], state.s[2 * b + 1][c]);
-#pragma unroll 1
+            float reach = reach0;
+#pragma unroll 2
             for (int it = 0; it < C / 16; ++it) {
                 f4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -113,8 +113,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || DK + DV == 128) ? 2 : 1) vo
                     fq.rows(tile_q, QS, 16 * it, 32 * b);
                     mma(o, fs[b], fq);
                 }
-                const int i = 16 * it + c16;
-                o *= power(l2, (float)(i + 1)) * scale;
+                o *= reach;
+                reach *= reach16;
 #pragma unroll
                 for (int b = 0; b < C / 32; ++b)
                     if (b <= it / 2) {
@@ -122,88 +122,163 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || DK + DV == 128) ? 2 : 1) vo
                         fp.rows(tile_p, PS, 16 * it, 32 * b);
                         mma(o, fv[b], fp);
                     }
-                if (i < n)
-                    store4(o0 + (t + i) * a.ld_o + col + 4 * g, dv - col - 4 * g, o);
+                const int i = 16 * it + c16;
+                if (i < tokens)
+                    store4<T, FULL>(o0 + (t + i) * a.ld_o + col + 4 * g, dv - col - 4 * g, o);
             }
         }
         phase();
-        state.template update<C>(tile_k, tile_v, w, power(l2, (float)n));
-        t += n;
-        if (t == seg.end) {
-            if (a.state_out) {
-                const int64_t row = state_row(a.slots, a.n_slots, seg.seq);
+        state.template update<C>(tile_k, tile_v, w, power(l2, (float)tokens));
+    };
+    // Tiles of the range, in order: rows t .. t + n - 1 of one sequence.
+    Segment seg;
+    seg.enter(seqs, rows.first, true);
+    const bool starts_here = seg.start >= rows.first;
+    struct Item {
+        int64_t t, seq;
+        int n;  // 0: none
+        bool first, last, behind;  // of its sequence's tiles in the range; the sequence leaves it
+    };
+    auto item = [&](int64_t t, bool first) -> Item {
+        const int64_t stop = seg.end < rows.end ? seg.end : rows.end;
+        const int n = stop - t < C ? (int)(stop - t) : C;
+        return {t, seg.seq, n, first, t + n == seg.end, seg.end > rows.end};
+    };
+    Item now = {}, next = item(rows.first, true);
+    while (true) {
+        if (next.n > 0)
+            load(next.t, next.n);  // on its way while the tile in LDS is worked on
+        if (now.n > 0) {
+            if (now.first) {
+                const float *p = nullptr;
+                if (now.t == rows.first && !starts_here)
+                    p = a.ends + ((range - 1) * a.in.H + h) * size;
+                else if (a.starts && now.behind)  // another workgroup may have written the slot
+                    p = a.starts + (range * a.in.H + h) * size;
+                else if (a.in.state_in) {
+                    const int64_t row = state_row(a.slots, a.n_slots, now.seq);
+                    p = row >= 0 ? a.in.state_in + (row * a.in.H + h) * size : nullptr;
+                }
+                state.load(p, dk, dv, dv, 1);
+            }
+            work(now.t, now.n);
+            if (now.last && a.state_out) {
+                const int64_t row = state_row(a.slots, a.n_slots, now.seq);
                 if (row >= 0)
                     state.store(a.state_out + (row * a.in.H + h) * size, dk, dv);
             }
-            if (t < rows.end) {
-                seg.advance(seqs);
-                begin();
-            }
         }
         __syncthreads();
+        if (next.n == 0)
+            return;
+        if (put() && next.n > 1) {  // a token by itself
+            next.n = 1;
+            next.last = next.t + 1 == seg.end;
+            now.n = 0;
+            continue;
+        }
+        now = next;
+        const int64_t t = now.t + now.n;
+        if (t >= rows.end) {
+            next.n = 0;
+        } else {
+            if (now.last)
+                seg.advance(seqs);
+            next = item(t, now.last);
+        }
     }
 }
 
-// What a range adds to the state of the sequence that passes its end (states), or to the gradient
-// of the state of the sequence that passes its start.
-template <typename T, int DK, int DV>
-__global__ __launch_bounds__(256) void ends_kernel(const AttentionArgs a, int64_t first,
-                                                   bool backward)
+// What a range adds to the state of the sequence that passes its end, or (backward) to the gradient
+// of the state of the sequence that passes its start.  With marks (the gradient's), also what the
+// range, or the sequence's first state, adds to the states before the second and further tiles of
+// each of its sequences.
+template <typename T, int DK, int DV, bool FULL>
+__global__ __launch_bounds__(256, resident<T>(DK + DV)) void ends_kernel(const AttentionArgs a,
+                                                                        int64_t first, bool backward,
+                                                                        int tile_rows, int marks)
 {
     constexpr int QS = tile_stride<T>(DK), VS = tile_stride<T>(DV);
     __shared__ __align__(16) T tile_a[C * QS], tile_b[C * VS];
     const int h = blockIdx.x % a.in.H, kh = h / (a.in.H / a.in.KH);
     const int64_t range = first + blockIdx.x / a.in.H;
-    const int dk = a.in.DK, dv = a.in.DV;
-    const int64_t size = (int64_t)dk * dv;
+    const int dk = FULL ? DK : a.in.DK, dv = FULL ? DV : a.in.DV;
+    const int64_t size = (int64_t)dk * dv, at = range * a.in.H + h;
     const float l2 = log2_decay(a.in.log_decay, h);
     const Sequences seqs = sequences_of(a.in);
     const Rows rows(a, range);
-    Segment seg;
-    seg.enter(seqs, backward ? rows.first : rows.end - 1, true);
-    const bool before = seg.start < rows.first, behind = seg.end > rows.end;
-    int32_t *flag = (backward ? a.head_flags : a.end_flags) + range;
-    if (backward ? !before : !behind) {
-        if (h == 0 && threadIdx.x == 0)
-            *flag = 0;
-        return;
-    }
-    if (h == 0 && threadIdx.x == 0)
-        *flag = before && behind ? kWhole : kPart;
-    const int64_t from = before ? rows.first : seg.start, to = behind ? rows.end : seg.end;
-    State<T, DK, DV> state;
+    const T *a0 = backward ? (const T *)a.in.q + h * dk : (const T *)a.in.k + kh * dk;
+    const T *b0 = backward ? (const T *)a.dout + h * dv : (const T *)a.in.v + kh * dv;
+    const int64_t ld_a = backward ? a.in.ld_q : a.in.ld_k;
+    const int64_t ld_b = backward ? a.ld_dout : a.in.ld_v;
+    State<T, DK, DV, FULL> state;
     float w[C / 4];
-    if (!backward) {
-        const int64_t row = !before && a.in.state_in ? state_row(a.slots, a.n_slots, seg.seq) : -1;
-        state.load(row >= 0 ? a.in.state_in + (row * a.in.H + h) * size : nullptr, dk, dv, dv, 1);
-        if (a.starts && !before)
-            state.store(a.starts + (range * a.in.H + h) * size, dk, dv);
-        const T *k0 = (const T *)a.in.k + kh * dk, *v0 = (const T *)a.in.v + kh * dv;
-        for (int64_t t = from; t < to; t += C) {
-            const int n = to - t < C ? (int)(to - t) : C;
-            load_tile<T, C, DK>(tile_a, k0 + t * a.in.ld_k, a.in.ld_k, n, dk);
-            load_tile<T, C, DV>(tile_b, v0 + t * a.in.ld_v, a.in.ld_v, n, dv);
-            if (t == from || n < C)
-                to_end<C>(w, l2, n);
-            __syncthreads();
-            state.template update<C>(tile_a, tile_b, w, power(l2, (float)n));
-            __syncthreads();
+    int weights_of = 0;
+    TileLoad<T, C, DK, FULL> next_a;
+    TileLoad<T, C, DV, FULL> next_b;
+    Segment seg;
+    seg.enter(seqs, backward || marks > 0 ? rows.first : rows.end - 1, true);
+    while (true) {
+        const bool before = seg.start < rows.first, behind = seg.end > rows.end;
+        const int64_t from = before ? rows.first : seg.start, to = behind ? rows.end : seg.end;
+        // one sequence passes the end, or the start; others matter for their marks only
+        const bool passes = a.cut.joined && (backward ? before : behind);
+        if (passes && h == 0 && threadIdx.x == 0)
+            (backward ? a.head_flags : a.end_flags)[range] = before && behind ? kWhole : kPart;
+        const float *begin = nullptr;
+        if (backward) {
+            if (!behind && a.dstate_out)
+                begin = a.dstate_out + (seg.seq * a.in.H + h) * size;
+        } else if (!before && a.in.state_in) {
+            const int64_t row = state_row(a.slots, a.n_slots, seg.seq);
+            begin = row >= 0 ? a.in.state_in + (row * a.in.H + h) * size : nullptr;
         }
-    } else {
-        state.load(!behind && a.dstate_out ? a.dstate_out + (seg.seq * a.in.H + h) * size : nullptr,
-                   dk, dv, dv, 1);
-        const T *q0 = (const T *)a.in.q + h * dk, *d0 = (const T *)a.dout + h * dv;
-        for (int64_t t = from + (to - from - 1) / C * C; t >= from; t -= C) {
-            const int n = to - t < C ? (int)(to - t) : C;
-            load_tile<T, C, DK>(tile_a, q0 + t * a.in.ld_q, a.in.ld_q, n, dk);
-            load_tile<T, C, DV>(tile_b, d0 + t * a.ld_dout, a.ld_dout, n, dv);
-            from_start<C>(w, l2, n, a.in.scale);
-            __syncthreads();
-            state.template update<C>(tile_a, tile_b, w, power(l2, (float)n));
-            __syncthreads();
+        // the last tile is for what passes only
+        const int tiles = (int)((to - from + tile_rows - 1) / tile_rows) - (passes ? 0 : 1);
+        if (tiles > 0) {
+            state.load(begin, dk, dv, dv, 1);
+            if (a.starts && passes && !before)
+                state.store(a.starts + at * size, dk, dv);
+            int n = 0;
+            int64_t t = 0;
+            auto load = [&](int i) {
+                t = from + (int64_t)(backward ? tiles - 1 - i : i) * tile_rows;
+                n = to - t < tile_rows ? (int)(to - t) : tile_rows;
+                next_a.load(a0 + t * ld_a, ld_a, n, dk);
+                next_b.load(b0 + t * ld_b, ld_b, n, dv);
+            };
+            load(0);
+            for (int i = 0; i < tiles; ++i) {
+                next_a.put(tile_a);
+                next_b.put(tile_b);
+                __syncthreads();
+                const int tokens = n;
+                const int64_t end = t + n;
+                if (i + 1 < tiles)
+                    load(i + 1);
+                if (tokens != weights_of) {
+                    if (backward)
+                        from_start<C>(w, l2, tokens, a.in.scale);
+                    else
+                        to_end<C>(w, l2, tokens);
+                    weights_of = tokens;
+                }
+                state.template update<C>(tile_a, tile_b, w, power(l2, (float)tokens));
+                if (marks > 0 && end < to)
+                    state.store(a.marks + (at * marks + (end - rows.first) / tile_rows - 1) * size,
+                                dk, dv);
+                __syncthreads();
+            }
+            if (passes)
+                state.store((backward ? a.heads : a.ends) + at * size, dk, dv);
         }
+        if (!passes && a.cut.joined && h == 0 && threadIdx.x == 0 &&
+            (backward || seg.end >= rows.end))
+            (backward ? a.head_flags : a.end_flags)[range] = 0;
+        if (marks == 0 || to >= rows.end)
+            return;
+        seg.advance(seqs);
     }
-    state.store((backward ? a.heads : a.ends) + (range * a.in.H + h) * size, dk, dv);
 }
 
 // States along the ranges of a sequence (of all tokens, with offsets), or their gradients against
@@ -259,8 +334,20 @@ __global__ __launch_bounds__(256) void empty_kernel(const AttentionArgs a, int64
         return;
     const float *from = backward ? a.dstate_out : a.in.state_in;
     float *to = (backward ? a.out.dstate_in : a.state_out) + (row * a.in.H + h) * size;
-    for (int64_t e = threadIdx.x; e < size; e += 256)
-        to[e] = from ? from[(row * a.in.H + h) * size + e] : 0.f;
+    if (from)
+        from += (row * a.in.H + h) * size;
+    constexpr int MOST = LBI_ATTENTION_MAX_DIM * LBI_ATTENTION_MAX_DIM / 2048;
+    float x[MOST][8];
+#pragma unroll
+    for (int i = 0; i < MOST; ++i) {
+        const int e = (i * 256 + threadIdx.x) * 8;
+        load_some<8>(from + (e < size ? e : 0), from ? (int)size - e : 0, x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < MOST; ++i) {
+        const int e = (i * 256 + threadIdx.x) * 8;
+        store_some<8>(to + (e < size ? e : 0), (int)size - e, x[i]);
+    }
 }
 
 // One token: a workgroup takes a head of a sequence, COLS lanes of 4 columns side by side, the
@@ -345,15 +432,17 @@ AttentionCut attention_cut(const lbi_attention_inputs &in, bool ragged)
     return c;
 }
 
-hipError_t launch_attention_ends(const AttentionArgs &a, bool backward, hipStream_t stream)
+hipError_t launch_attention_ends(const AttentionArgs &a, bool backward, int tile_rows, int marks,
+                                 hipStream_t stream)
 {
-    hipError_t e = by_head(a.in, [&](auto type, auto dk, auto dv) {
+    hipError_t e = by_head(a.in, [&](auto type, auto dk, auto dv, auto full) {
         return in_launches(a.cut.ranges, a.in.H, [&](int64_t first, dim3 grid) {
-            ends_kernel<decltype(type), decltype(dk)::value, decltype(dv)::value>
-                <<<grid, 256, 0, stream>>>(a, first, backward);
+            ends_kernel<decltype(type), decltype(dk)::value, decltype(dv)::value,
+                        decltype(full)::value>
+                <<<grid, 256, 0, stream>>>(a, first, backward, tile_rows, marks);
         });
     });
-    if (e != hipSuccess)
+    if (e != hipSuccess || !a.cut.joined)
         return e;
     const int64_t size = (int64_t)a.in.DK * a.in.DV;
     const int blocks = (int)((size + 255) / 256);
@@ -375,11 +464,12 @@ hipError_t launch_linear_attention(const AttentionArgs &a, hipStream_t stream)
     hipError_t e = hipSuccess;
     if (a.in.T > 0) {
         if (a.cut.joined)
-            e = launch_attention_ends(a, false, stream);
+            e = launch_attention_ends(a, false, C, 0, stream);
         if (e == hipSuccess)
-            e = by_head(a.in, [&](auto type, auto dk, auto dv) {
+            e = by_head(a.in, [&](auto type, auto dk, auto dv, auto full) {
                 return in_launches(a.cut.ranges, a.in.H, [&](int64_t first, dim3 grid) {
-                    attention_kernel<decltype(type), decltype(dk)::value, decltype(dv)::value>
+                    attention_kernel<decltype(type), decltype(dk)::value, decltype(dv)::value,
+                        decltype(full)::value>
                         <<<grid, 256, 0, stream>>>(a, first);
                 });
             });

@@ -19,25 +19,38 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 
 // ---- matrix operands
 
+// Tiles of bf16 in LDS have the two halves of every 16 values exchanged in rows 8 .. 15 of 16, at
+// a stride of 32 bytes more than their values: the 32 lanes that LDS serves together then touch
+// all its banks once, reading rows and reading columns.  Float32 tiles lie as they are.
+template <typename T> __device__ __forceinline__ int swapped(int row)
+{
+    return sizeof(T) == 2 ? row & 8 : 0;
+}
+template <typename T> constexpr int tile_stride(int values) { return values + (sizeof(T) == 2 ? 16 : 4); }
+// Where this lane's four values 4 g .. of 16 lie in row c of 16.
+template <typename T> __device__ __forceinline__ int lane_quad()
+{
+    return 4 * (threadIdx.x >> 4 & 3) ^ swapped<T>(threadIdx.x & 15);
+}
+
 template <typename T> struct Frag;
 template <> struct Frag<bf16_bits> {
     u4 w;  // pairs: k = 4 g + (0, 1), (2, 3), 16 + 4 g + (0, 1), (2, 3)
 
-    // Of a matrix stored [row][k]: lane c takes row `row0` + c.
+    // Of a tile [row][k]: lane c takes row `row0` + c.
     __device__ __forceinline__ void rows(const bf16_bits *m, int stride, int row0, int k0)
     {
-        const int lane = threadIdx.x & 63;
-        const bf16_bits *p = m + (row0 + (lane & 15)) * stride + k0 + 4 * (lane >> 4);
+        const int c = threadIdx.x & 15;
+        const bf16_bits *p = m + (row0 + c) * stride + k0 + lane_quad<bf16_bits>();
         const u2 a = *(const u2 *)p, b = *(const u2 *)(p + 16);
         w = u4{a.x, a.y, b.x, b.y};
     }
-    // Of a matrix stored [k][col]: lane c takes column `col0` + c.  The hardware's transposing
-    // read: sixteen lanes give the addresses of 4 rows of 16 values, four lanes a row, and get a
-    // column of 4 each.
+    // Of a tile [k][col]: lane c takes column `col0` + c.  The hardware's transposing read: sixteen
+    // lanes give the addresses of 4 rows of 16 values, four lanes a row, and get a column of 4 each.
     __device__ __forceinline__ void cols(const bf16_bits *m, int stride, int k0, int col0)
     {
-        const int lane = threadIdx.x & 63, c = lane & 15;
-        const bf16_bits *p = m + (k0 + 4 * (lane >> 4) + (c >> 2)) * stride + col0 + 4 * (c & 3);
+        const int c = threadIdx.x & 15, g = threadIdx.x >> 4 & 3;
+        const bf16_bits *p = m + (k0 + 4 * g + (c >> 2)) * stride + col0 + (4 * (c & 3) ^ (4 * g & 8));
         typedef __attribute__((address_space(3))) s4 lds_s4;
         const u2 a = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)p));
         const u2 b = __builtin_bit_cast(
@@ -174,38 +187,69 @@ __device__ __forceinline__ float power(float l2, float n) { return __builtin_amd
 
 // ---- tiles of tokens in LDS
 
-// Elements from one row of a tile to the next: 16 bytes more than its values, so that 16-byte
-// pieces of eight rows lie in different banks.
-template <typename T> constexpr int tile_stride(int values) { return values + 16 / (int)sizeof(T); }
+// Kernels come in two forms.  FULL: a head's keys and values fill the tiles' widths, so whole vectors
+// are loaded and stored; otherwise every vector may end early, and the code for that is several times
+// as long as the rest.
 
-// Rows first .. first + n - 1 of a token tensor (n <= C), `values` of a head each, into m
-// [C][tile_stride(W)]; zeros behind them.  True where a value is infinite or NaN.
-template <typename T, int C, int W>
-__device__ __forceinline__ bool load_tile(T *m, const T *p, int64_t ld, int n, int values)
-{
-    bool bad = false;
-    constexpr int PER_ROW = W / 8, STRIDE = tile_stride<T>(W);
+// Rows of a token tensor on their way into a tile [C][tile_stride(W)]: `values` of a head of each
+// of n <= C tokens, zeros behind them.  Loads stay in flight until put().
+template <typename T, int C, int W, bool FULL> struct TileLoad {
+    static constexpr int COUNT = C * W / 2048, STEP = 2048 / W;  // rows between a thread's pieces
+    Raw<T, 8> r[COUNT];
+
+    __device__ __forceinline__ static int row() { return threadIdx.x / (W / 8); }
+    __device__ __forceinline__ static int col() { return threadIdx.x % (W / 8) * 8; }
+    // p, ld and n are the same in all threads; n > 0
+    __device__ __forceinline__ void load(const T *p, int64_t ld, int n, int values)
+    {
+        p = uniform_pointer(p);
 #pragma unroll
-    for (int i = 0; i < C * PER_ROW / 256; ++i) {
-        const int at = i * 256 + threadIdx.x, row = at / PER_ROW, col = at % PER_ROW * 8;
-        Raw<T, 8> r;
-        r.load(p + (row < n ? row : 0) * ld + col, row < n ? values - col : 0);
-        T *to = m + row * STRIDE + col;
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                bad |= (r.w[k] & 0x7F80u) == 0x7F80u || (r.w[k] & 0x7F800000u) == 0x7F800000u;
-            *(u4 *)to = u4{r.w[0], r.w[1], r.w[2], r.w[3]};
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                bad |= (fbits(r.v[k]) & 0x7F800000u) == 0x7F800000u;
-            *(f4 *)to = f4{r.v[0], r.v[1], r.v[2], r.v[3]};
-            *(f4 *)(to + 4) = f4{r.v[4], r.v[5], r.v[6], r.v[7]};
+        for (int i = 0; i < COUNT; ++i) {
+            const int at = row() + i * STEP;
+            const uint32_t bytes = (uint32_t)((at < n ? at : 0) * (int)ld + col()) * (uint32_t)sizeof(T);
+            if constexpr (FULL) {
+                r[i].load(lane_address(p, bytes), 8);
+                r[i].keep(at < n);
+            } else {
+                r[i].load(lane_address(p, bytes), at < n ? values - col() : 0);
+            }
         }
     }
-    return bad;
-}
+    // True where a value is infinite or NaN.
+    __device__ __forceinline__ bool put(T *m) const
+    {
+        if constexpr (sizeof(T) == 2) {
+            typedef unsigned short h2 __attribute__((ext_vector_type(2)));
+            typedef short i2 __attribute__((ext_vector_type(2)));
+            h2 high = {0, 0};  // largest bits of negative values
+            i2 low = {0, 0};   // and of positive ones
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                const int at = row() + i * STEP;
+                *(u4 *)(m + at * tile_stride<T>(W) + (col() ^ swapped<T>(at))) =
+                    u4{r[i].w[0], r[i].w[1], r[i].w[2], r[i].w[3]};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    high = __builtin_elementwise_max(high, __builtin_bit_cast(h2, r[i].w[k]));
+                    low = __builtin_elementwise_max(low, __builtin_bit_cast(i2, r[i].w[k]));
+                }
+            }
+            return high.x >= 0xFF80 || high.y >= 0xFF80 || low.x >= 0x7F80 || low.y >= 0x7F80;
+        } else {
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                T *to = m + (row() + i * STEP) * tile_stride<T>(W) + col();
+                *(f4 *)to = f4{r[i].v[0], r[i].v[1], r[i].v[2], r[i].v[3]};
+                *(f4 *)(to + 4) = f4{r[i].v[4], r[i].v[5], r[i].v[6], r[i].v[7]};
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    top = umax(top, fbits(r[i].v[k]) & 0x7FFFFFFFu);
+            }
+            return top >= 0x7F800000u;
+        }
+    }
+};
 // A barrier, and whether any thread of the workgroup said `bad`.
 __device__ __forceinline__ bool any_bad(bool bad, int *flags)
 {
@@ -220,7 +264,7 @@ __device__ __forceinline__ bool any_bad(bool bad, int *flags)
 
 // The state [DK][DV] of a head in registers: wavefront w has columns w DV / 4 .. of it, in 16 x 16
 // results.  (With DK and DV exchanged: its transpose.)
-template <typename T, int DK, int DV> struct State {
+template <typename T, int DK, int DV, bool FULL> struct State {
     static constexpr int KT = DK / 16, VT = DV / 64;
     f4 s[KT][VT];
 
@@ -242,9 +286,9 @@ template <typename T, int DK, int DV> struct State {
     __device__ __forceinline__ void each(P *p, int dk, int dv, int row, int col, F &&f)
     {
         const int lane = threadIdx.x & 63, i0 = 4 * (lane >> 4), j0 = column(0) + (lane & 15);
-        p = (P *)uniform((int64_t)p);
+        p = uniform_pointer(p);
         const uint32_t base = (uint32_t)(i0 * row + j0 * col) * 4;
-        const bool whole = dk == DK && dv == DV;
+        const bool whole = FULL || (dk == DK && dv == DV);
 #pragma unroll
         for (int k = 0; k < KT; ++k)
 #pragma unroll
@@ -350,11 +394,11 @@ struct Rows {
 };
 
 // 4 consecutive values of a token's row
-template <typename T>
+template <typename T, bool FULL = false>
 __device__ __forceinline__ void store4(T *p, int left, const f4 &v)
 {
     const float x[4] = {v.x, v.y, v.z, v.w};
-    store_some<4>(p, left, x);
+    store_some<4>(p, FULL ? 4 : left, x);
 }
 // ... into a tile
 __device__ __forceinline__ void put4(bf16_bits *p, const f4 &v)
@@ -371,28 +415,49 @@ __device__ __forceinline__ f4 get4(const bf16_bits *p)
 __device__ __forceinline__ f4 get4(const float *p) { return *(const f4 *)p; }
 
 // The 16 x 16 tiles (row, column) of a tile's C x C products of queries and keys that are needed,
-// dealt to the wavefronts: f(row, column) for column <= row, and for those beside the diagonal
-// that operands of 32 read as zeros (column = row + 1, row even).
+// dealt to the wavefronts: f(which, row, column) for column <= row, and for those beside the
+// diagonal that operands of 32 read as zeros (column = row + 1, row even).
+template <int C> constexpr int kCausalTiles = C == 64 ? 3 : 1;  // of a wavefront
 template <int C, typename F> __device__ __forceinline__ void causal_tiles(F &&f)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll 1
-    for (int at = 0; at < (C == 64 ? 3 : 1); ++at)
-        f(at == 0 ? wave >> 1 : at + 1, at == 0 ? wave & 1 : wave);
+#pragma unroll
+    for (int at = 0; at < kCausalTiles<C>; ++at)
+        f(at, at == 0 ? wave >> 1 : at + 1, at == 0 ? wave & 1 : wave);
+}
+// scale a^(i-j) at this lane's places of those tiles, 0 for j > i.
+template <int C>
+__device__ __forceinline__ void causal_fade(f4 (&fade)[kCausalTiles<C>], float l2, float scale)
+{
+    causal_tiles<C>([&](int at, int it, int jt) {
+        const int lag = 16 * (it - jt) + (threadIdx.x & 15) - 4 * (threadIdx.x >> 4 & 3);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            fade[at][r] = lag >= r ? power(l2, (float)(lag - r)) * scale : 0.f;
+    });
 }
 
 // Between phases that take the same operands from LDS: they are loaded again rather than kept.
-__device__ __forceinline__ void phase() { asm volatile("" ::: "memory"); }
+__device__ __forceinline__ void phase()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 
-// Calls f(type, DK, DV) with the storage type and the tiles' widths for the head's.
+// Calls f(type, DK, DV, FULL) with the storage type and the tiles' widths for the head's.
 template <typename F> hipError_t by_head(const lbi_attention_inputs &in, F &&f)
 {
     using W64 = std::integral_constant<int, 64>;
     using W128 = std::integral_constant<int, 128>;
+    auto full = [&](auto type, auto dk, auto dv) {
+        if (in.DK == decltype(dk)::value && in.DV == decltype(dv)::value)
+            return f(type, dk, dv, std::true_type{});
+        return f(type, dk, dv, std::false_type{});
+    };
     auto widths = [&](auto type) {
         if (in.DK <= 64)
-            return in.DV <= 64 ? f(type, W64{}, W64{}) : f(type, W64{}, W128{});
-        return in.DV <= 64 ? f(type, W128{}, W64{}) : f(type, W128{}, W128{});
+            return in.DV <= 64 ? full(type, W64{}, W64{}) : full(type, W64{}, W128{});
+        return in.DV <= 64 ? full(type, W128{}, W64{}) : full(type, W128{}, W128{});
     };
     return in.dt == LBI_BF16 ? widths(bf16_bits{}) : widths(float{});
 }

@@ -13,10 +13,10 @@
 // The last line differentiates every power of a where it stands, so that nothing in it cancels;
 // it is formed from float32 sums of products of the inputs themselves.
 //
-// A workgroup takes a head along a range of tokens, twice: forwards for the states before its
-// tiles, which it keeps in memory, then backwards with everything else.  G is held in both
-// layouts, as the operand of G v and of G^T k.  States at the ranges' starts and gradients at
-// their ends come from the kernels of the forward pass.
+// A first kernel walks forwards along each range of tokens and leaves the states before its tiles
+// in memory; then a workgroup takes a head along a range backwards with everything else.  G is
+// held in both layouts, as the operand of G v and of G^T k.  The states that enter the ranges and
+// the gradients that leave them are carried as in the forward pass.
 #include "lbi_attention.hpp"
 
 namespace lbi {
@@ -26,9 +26,9 @@ namespace {
 template <typename T, int DK, int DV>
 constexpr int tile_tokens() { return sizeof(T) == 4 && DK + DV == 256 ? 32 : 64; }
 
-template <typename T, int DK, int DV>
-__global__ __launch_bounds__(256) void attention_backward_kernel(const AttentionArgs a,
-                                                                 int64_t first, int marks)
+template <typename T, int DK, int DV, bool FULL>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && DK + DV == 128 ? 2 : 1) void
+attention_backward_kernel(const AttentionArgs a, int64_t first, int marks)
 {
     constexpr int C = tile_tokens<T, DK, DV>();
     constexpr int QS = tile_stride<T>(DK), VS = tile_stride<T>(DV), PS = tile_stride<T>(C);
@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256) void attention_backward_kernel(const Attention
     const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
     const int h = blockIdx.x % a.in.H, kh = h / (a.in.H / a.in.KH);
     const int64_t range = first + blockIdx.x / a.in.H;
-    const int dk = a.in.DK, dv = a.in.DV;
+    const int dk = FULL ? DK : a.in.DK, dv = FULL ? DV : a.in.DV;
     const int64_t size = (int64_t)dk * dv;
     const float l2 = log2_decay(a.in.log_decay, h), scale = a.in.scale;
     const T *q0 = (const T *)a.in.q + h * dk, *k0 = (const T *)a.in.k + kh * dk;
@@ -50,46 +50,40 @@ __global__ __launch_bounds__(256) void attention_backward_kernel(const Attention
 
     const Sequences seqs = sequences_of(a.in);
     const Rows rows(a, range);
-    Segment seg;
-    auto state_in = [&](int64_t seq) {
-        return a.in.state_in ? a.in.state_in + (seq * a.in.H + h) * size : nullptr;
-    };
-    // the state before the first tile of the segment that begins in the range at row `lo`
-    auto begin = [&](int64_t lo) -> const float * {
-        return seg.start < lo ? a.ends + ((range - 1) * a.in.H + h) * size : state_in(seg.seq);
-    };
-    State<T, DK, DV> state;
     float w[C / 4];
-
-    // forwards: the states before the second and further tiles of each sequence
-    seg.enter(seqs, rows.first, true);
-    for (int64_t lo = rows.first; lo < rows.end;) {
-        const int64_t hi = seg.end < rows.end ? seg.end : rows.end;
-        if (hi - lo > C) {
-            state.load(begin(lo), dk, dv, dv, 1);
-            to_end<C>(w, l2, C);
-            for (int64_t t = lo; t + C < hi; t += C) {
-                load_tile<T, C, DK>(tile_k, k0 + t * a.in.ld_k, a.in.ld_k, C, dk);
-                load_tile<T, C, DV>(tile_v, v0 + t * a.in.ld_v, a.in.ld_v, C, dv);
-                __syncthreads();
-                state.template update<C>(tile_k, tile_v, w, power(l2, (float)C));
-                state.store(mark0 + ((t + C - rows.first) / C - 1) * size, dk, dv);
-                __syncthreads();
-            }
-        }
-        lo = hi;
-        if (lo < rows.end)
-            seg.advance(seqs);
-    }
-    __syncthreads();
-
-    State<T, DK, DV> gb;  // G [dk][dv], a wavefront some columns dv
-    State<T, DV, DK> ga;  // its transpose
+    State<T, DK, DV, FULL> gb;  // G [dk][dv], a wavefront some columns dv
+    State<T, DV, DK, FULL> ga;  // its transpose
     float decay = 0.f, decay_state = 0.f;
+    f4 causal[kCausalTiles<C>];
+    causal_fade<C>(causal, l2, scale);
 
-    // Tokens t .. t + n - 1 whose tiles are loaded, from the state at `before` ([dk][dv]).
-    auto tile = [&](int64_t t, int n, const float *before) {
-        causal_tiles<C>([&](int it, int jt) {
+    // The state before a tile: what its range or its sequence's first state adds, and what enters
+    // the range; either may be NULL.
+    struct Before {
+        const float *own, *entering;
+        float fade;  // of what enters
+    };
+
+    // This wavefront's part of that state as the operand of S do, from column c on.
+    auto fetch = [&](const Before &b, int c, float (&x)[DV / 16][4], float (&y)[DV / 16][4]) {
+        const int row = ga.column(c) + c16;
+#pragma unroll
+        for (int u = 0; u < DV / 16; ++u) {
+            const int at = 16 * u + 4 * g, left = FULL ? 4 : row < dk ? dv - at : 0;
+            load_some<4>(b.own + row * dv + at, b.own ? left : 0, x[u]);
+            load_some<4>(b.entering + row * dv + at, b.entering ? left : 0, y[u]);
+        }
+    };
+
+    // With keys or values of 128 the registers do not hold what is on its way as well.
+    constexpr bool AHEAD = FULL && DK + DV == 128;
+
+    // Tokens t .. t + n - 1 whose tiles are loaded.
+    auto tile = [&](int64_t t, int n, const Before &before) {
+        float own[DV / 16][4], entering[DV / 16][4];
+        if (AHEAD)
+            fetch(before, 0, own, entering);
+        causal_tiles<C>([&](int at, int it, int jt) {
             f4 p = {0.f, 0.f, 0.f, 0.f}, e = {0.f, 0.f, 0.f, 0.f};
             if (jt <= it) {
 #pragma unroll
@@ -109,15 +103,14 @@ __global__ __launch_bounds__(256) void attention_backward_kernel(const Attention
                 const int lag = 16 * (it - jt) + c16 - 4 * g;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float fade = power(l2, (float)(lag - r)) * scale;
-                    p[r] = lag >= r ? p[r] * fade : 0.f;
+                    p[r] = lag >= r ? p[r] * causal[at][r] : 0.f;
                     decay += lag >= r ? (float)(lag - r) * p[r] * e[r] : 0.f;
-                    e[r] = lag >= r ? e[r] * fade : 0.f;
+                    e[r] = lag >= r ? e[r] * causal[at][r] : 0.f;
                 }
             }
-            const int at = (16 * it + c16) * PS + 16 * jt + 4 * g;
-            put4(tile_p + at, p);
-            put4(tile_e + at, e);
+            const int to = (16 * it + c16) * PS + 16 * jt + lane_quad<T>();
+            put4(tile_p + to, p);
+            put4(tile_e + to, e);
         });
         __syncthreads();
         const float fade = power(l2, (float)n);
@@ -125,23 +118,23 @@ __global__ __launch_bounds__(256) void attention_backward_kernel(const Attention
         for (int c = 0; c < DK / 64; ++c) {
             const int col = ga.column(c);
             {   // dq
+                if (!AHEAD)
+                    fetch(before, c, own, entering);
                 Wide<T, 2> fs[DV / 32];
+                float inner = 0.f;
 #pragma unroll
                 for (int b = 0; b < DV / 32; ++b) {
                     f4 x[2];
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int at = 32 * b + 16 * u + 4 * g;
-                        float y[4];
-                        load_some<4>(before + (col + c16) * dv + at,
-                                     before && col + c16 < dk ? dv - at : 0, y);
-                        x[u] = f4{y[0], y[1], y[2], y[3]};
+                    for (int u = 0; u < 2; ++u)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            decay_state += (float)n * fade * y[r] * ga.s[2 * b + u][c][r];
-                    }
+                        for (int r = 0; r < 4; ++r) {
+                            x[u][r] = own[2 * b + u][r] + before.fade * entering[2 * b + u][r];
+                            inner += x[u][r] * ga.s[2 * b + u][c][r];
+                        }
                     pack_tiles(fs[b], x[0], x[1]);
                 }
+                decay_state += (float)n * fade * inner;
                 Frag<T> fk[C / 32];
 #pragma unroll
                 for (int b = 0; b < C / 32; ++b)
@@ -157,7 +150,7 @@ __global__ __launch_bounds__(256) void attention_backward_kernel(const Attention
                     }
                     const int i = 16 * it + c16;
                     x *= power(l2, (float)(i + 1)) * scale;
-                    const f4 q = get4(tile_q + i * QS + col + 4 * g);
+                    const f4 q = get4(tile_q + i * QS + col + lane_quad<T>());
                     decay += (float)(i + 1) * (x.x * q.x + x.y * q.y + x.z * q.z + x.w * q.w);
 #pragma unroll
                     for (int b = 0; b < C / 32; ++b)
@@ -167,7 +160,7 @@ __global__ __launch_bounds__(256) void attention_backward_kernel(const Attention
                             mma(x, fk[b], y);
                         }
                     if (i < n)
-                        store4(dq0 + (t + i) * a.out.ld_dq + col + 4 * g, dk - col - 4 * g, x);
+                        store4<T, FULL>(dq0 + (t + i) * a.out.ld_dq + col + 4 * g, dk - col - 4 * g, x);
                 }
             }
             phase();
@@ -192,7 +185,7 @@ __global__ __launch_bounds__(256) void attention_backward_kernel(const Attention
                     const int j = 16 * jt + c16;
                     const float left = (float)(n - 1 - j);
                     x *= j < n ? power(l2, left) : 0.f;
-                    const f4 k = get4(tile_k + j * QS + col + 4 * g);
+                    const f4 k = get4(tile_k + j * QS + col + lane_quad<T>());
                     decay += j < n ? left * (x.x * k.x + x.y * k.y + x.z * k.z + x.w * k.w) : 0.f;
 #pragma unroll
                     for (int b = 0; b < C / 32; ++b)
@@ -204,10 +197,10 @@ __global__ __launch_bounds__(256) void attention_backward_kernel(const Attention
                     if (j >= n)
                         continue;
                     if (shared)
-                        store4(a.part_k + ((t + j) * a.in.H + h) * dk + col + 4 * g,
+                        store4<float, FULL>(a.part_k + ((t + j) * a.in.H + h) * dk + col + 4 * g,
                                dk - col - 4 * g, x);
                     else
-                        store4((T *)a.out.dk + (t + j) * a.out.ld_dk + kh * dk + col + 4 * g,
+                        store4<T, FULL>((T *)a.out.dk + (t + j) * a.out.ld_dk + kh * dk + col + 4 * g,
                                dk - col - 4 * g, x);
                 }
             }
@@ -245,10 +238,10 @@ __global__ __launch_bounds__(256) void attention_backward_kernel(const Attention
                 if (j >= n)
                     continue;
                 if (shared)
-                    store4(a.part_v + ((t + j) * a.in.H + h) * dv + col + 4 * g, dv - col - 4 * g,
+                    store4<float, FULL>(a.part_v + ((t + j) * a.in.H + h) * dv + col + 4 * g, dv - col - 4 * g,
                            x);
                 else
-                    store4((T *)a.out.dv + (t + j) * a.out.ld_dv + kh * dv + col + 4 * g,
+                    store4<T, FULL>((T *)a.out.dv + (t + j) * a.out.ld_dv + kh * dv + col + 4 * g,
                            dv - col - 4 * g, x);
             }
         }
@@ -259,54 +252,127 @@ __global__ __launch_bounds__(256) void attention_backward_kernel(const Attention
         gb.template update<C>(tile_q, tile_d, w, fade);
         __syncthreads();
     };
+    TileLoad<T, C, DK, FULL> next_q, next_k;
+    TileLoad<T, C, DV, FULL> next_v, next_d;
     auto load = [&](int64_t t, int n) {
-        bool bad = load_tile<T, C, DK>(tile_q, q0 + t * a.in.ld_q, a.in.ld_q, n, dk);
-        bad |= load_tile<T, C, DK>(tile_k, k0 + t * a.in.ld_k, a.in.ld_k, n, dk);
-        bad |= load_tile<T, C, DV>(tile_v, v0 + t * a.in.ld_v, a.in.ld_v, n, dv);
-        bad |= load_tile<T, C, DV>(tile_d, d0 + t * a.ld_dout, a.ld_dout, n, dv);
+        next_q.load(q0 + t * a.in.ld_q, a.in.ld_q, n, dk);
+        next_k.load(k0 + t * a.in.ld_k, a.in.ld_k, n, dk);
+        next_v.load(v0 + t * a.in.ld_v, a.in.ld_v, n, dv);
+        next_d.load(d0 + t * a.ld_dout, a.ld_dout, n, dv);
+    };
+    auto put = [&] {
+        bool bad = next_q.put(tile_q);
+        bad |= next_k.put(tile_k);
+        bad |= next_v.put(tile_v);
+        bad |= next_d.put(tile_d);
         return any_bad(bad, flags);
     };
-
-    // backwards
-    seg.enter(seqs, rows.end - 1, true);
-    for (int64_t hi = rows.end; hi > rows.first;) {
-        const int64_t lo = seg.start < rows.first ? rows.first : seg.start;
-        const float *g0 = seg.end > rows.end
-                              ? a.heads + ((range + 1) * a.in.H + h) * size
-                              : (a.dstate_out ? a.dstate_out + (seg.seq * a.in.H + h) * size : nullptr);
-        gb.load(g0, dk, dv, dv, 1);
-        ga.load(g0, dv, dk, 1, dv);
-        for (int64_t t = lo + (hi - lo - 1) / C * C; t >= lo; t -= C) {
-            const int n = hi - t < C ? (int)(hi - t) : C;
-            const float *before =
-                t > lo ? mark0 + ((t - rows.first) / C - 1) * size : begin(lo);
-            // Where a value is infinite or NaN: token by token, each from the state that the ones
-            // before it in the tile leave, which 0 times it must not reach.
-            const bool bad = load(t, n);
-            float *scratch = mark0 + (int64_t)(marks - 1) * size;
-            for (int i = bad ? n - 1 : 0; i >= 0; --i) {
-                const float *from = before;
-                if (bad) {
-                    __syncthreads();
-                    if (i > 0) {
-                        load(t, i);
-                        state.load(before, dk, dv, dv, 1);
-                        to_end<C>(w, l2, i);
-                        state.template update<C>(tile_k, tile_v, w, power(l2, (float)i));
-                        state.store(scratch, dk, dv);
-                        from = scratch;
-                        __syncthreads();
-                    }
-                    load(t + i, 1);
-                }
-                tile(t + i, bad ? 1 : n, from);
-            }
-        }
-        if (lo == seg.start && a.out.dstate_in)
-            gb.store(a.out.dstate_in + (seg.seq * a.in.H + h) * size, dk, dv);
-        hi = lo;
-        if (hi > rows.first)
+    // The tiles from the range's end to its start: rows t .. t + n - 1 of seg, which has the rows
+    // from lo on in the range.
+    Segment seg;
+    int64_t lo = rows.end, t = rows.end;
+    enum Kind { kNone, kTile, kState };
+    struct Item {
+        Kind kind;
+        int64_t t, seq;
+        int n;
+        bool fresh, begins, behind;  // its sequence's last rows, its first ones; it leaves the range
+        Before before;
+    };
+    auto step = [&]() -> Item {
+        if (t <= rows.first)
+            return {};
+        Item x;
+        x.kind = kTile;
+        x.fresh = t == lo;
+        if (t > lo) {
+            t -= C;
+            x.n = C;
+        } else {
+            const int64_t hi = lo;
             seg.enter(seqs, hi - 1, true);
+            lo = seg.start < rows.first ? rows.first : seg.start;
+            t = lo + (hi - lo - 1) / C * C;
+            x.n = (int)(hi - t);
+        }
+        x.t = t;
+        x.seq = seg.seq;
+        x.begins = t == lo && lo == seg.start;
+        x.behind = seg.end > rows.end;
+        x.before = {nullptr, nullptr, power(l2, (float)(t - lo))};
+        if (t > lo)
+            x.before.own = mark0 + ((t - rows.first) / C - 1) * size;
+        else if (lo == seg.start && a.in.state_in)
+            x.before.own = a.in.state_in + (seg.seq * a.in.H + h) * size;
+        if (seg.start < lo)
+            x.before.entering = a.ends + ((range - 1) * a.in.H + h) * size;
+        return x;
+    };
+    // A tile with a value that is infinite or NaN is taken token by token, the last one first, each
+    // from the state that the ones before it in the tile leave, which 0 times it must not reach: for
+    // that state their rows are loaded once (kState), then the token itself.
+    float *scratch = mark0 + (int64_t)(marks - 1) * size;
+    Item now = {}, next = step(), whole = {};
+    int single = -1;  // the token of `whole` that is next
+    while (true) {
+        if (AHEAD && next.kind != kNone)
+            load(next.t, next.n);  // on its way while the tile in LDS is worked on
+        if (now.kind == kTile) {
+            if (now.fresh) {
+                const float *p = now.behind       ? a.heads + ((range + 1) * a.in.H + h) * size
+                                 : a.dstate_out ? a.dstate_out + (now.seq * a.in.H + h) * size
+                                                : nullptr;
+                gb.load(p, dk, dv, dv, 1);
+                ga.load(p, dv, dk, 1, dv);
+            }
+            tile(now.t, now.n, now.before);
+            if (now.begins && a.out.dstate_in)
+                gb.store(a.out.dstate_in + (now.seq * a.in.H + h) * size, dk, dv);
+        } else {
+            if (now.kind == kState) {
+                State<T, DK, DV, FULL> state, entering;
+                state.load(whole.before.own, dk, dv, dv, 1);
+                entering.load(whole.before.entering, dk, dv, dv, 1);
+                to_end<C>(w, l2, now.n);
+#pragma unroll
+                for (int x = 0; x < state.KT; ++x)
+#pragma unroll
+                    for (int y = 0; y < state.VT; ++y)
+                        state.s[x][y] += entering.s[x][y] * whole.before.fade;
+                state.template update<C>(tile_k, tile_v, w, power(l2, (float)now.n));
+                state.store(scratch, dk, dv);
+            }
+            __syncthreads();
+        }
+        if (next.kind == kNone)
+            break;
+        if (!AHEAD)
+            load(next.t, next.n);
+        const bool bad = put();
+        now = next;
+        if (bad && now.kind == kTile && now.n > 1) {
+            whole = now;
+            single = now.n - 1;
+            now.kind = kNone;
+        } else if (now.kind == kTile) {
+            --single;
+        }
+        if (single > 0 && now.kind != kState) {
+            next.kind = kState;
+            next.t = whole.t;
+            next.n = single;
+        } else if (single >= 0) {
+            next = whole;
+            next.t += single;
+            next.n = 1;
+            next.fresh = whole.fresh && single == whole.n - 1;
+            next.begins = whole.begins && single == 0;
+            if (single > 0)
+                next.before = {scratch, nullptr, 0.f};
+        } else {
+            single = -1;
+            next = step();
+        }
     }
     if (!a.part_decay)
         return;
@@ -347,7 +413,7 @@ struct ToVector {
 int64_t attention_marks(const lbi_attention_inputs &in, const AttentionCut &cut)
 {
     int64_t marks = 0;
-    (void)by_head(in, [&](auto type, auto dk, auto dv) {
+    (void)by_head(in, [&](auto type, auto dk, auto dv, auto full) {
         marks = cut.tokens /
                 tile_tokens<decltype(type), decltype(dk)::value, decltype(dv)::value>();
         return hipSuccess;
@@ -359,18 +425,17 @@ hipError_t launch_linear_attention_backward(const AttentionArgs &a, hipStream_t 
 {
     hipError_t e = hipSuccess;
     if (a.in.T > 0) {
-        if (a.cut.joined) {
-            e = launch_attention_ends(a, false, stream);
-            if (e == hipSuccess)
-                e = launch_attention_ends(a, true, stream);
-        }
+        const int marks = (int)attention_marks(a.in, a.cut);
+        const int tile_rows = (int)(a.cut.tokens / marks);
+        e = launch_attention_ends(a, false, tile_rows, marks, stream);
+        if (e == hipSuccess && a.cut.joined)
+            e = launch_attention_ends(a, true, kAttentionTile, 0, stream);
         if (e == hipSuccess)
-            e = by_head(a.in, [&](auto type, auto dk, auto dv) {
+            e = by_head(a.in, [&](auto type, auto dk, auto dv, auto full) {
                 using T = decltype(type);
                 constexpr int DK = decltype(dk)::value, DV = decltype(dv)::value;
-                const int marks = (int)attention_marks(a.in, a.cut);
                 return in_launches(a.cut.ranges, a.in.H, [&](int64_t first, dim3 grid) {
-                    attention_backward_kernel<T, DK, DV><<<grid, 256, 0, stream>>>(a, first, marks);
+                    attention_backward_kernel<T, DK, DV, decltype(full)::value><<<grid, 256, 0, stream>>>(a, first, marks);
                 });
             });
         if (e != hipSuccess)

@@ -61,6 +61,12 @@ template <int V> struct Raw<float, V> {
                 v[i] = i < n ? p[i] : 0.f;
         }
     }
+    __device__ __forceinline__ void keep(bool there)  // zeros otherwise
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            v[i] = there ? v[i] : 0.f;
+    }
     __device__ __forceinline__ void unpack(float (&x)[V]) const
     {
 #pragma unroll
@@ -88,6 +94,12 @@ template <int V> struct Raw<bf16_bits, V> {
                 w[i] = (2 * i < n ? (uint32_t)p[2 * i] : 0u) |
                        (2 * i + 1 < n ? (uint32_t)p[2 * i + 1] << 16 : 0u);
         }
+    }
+    __device__ __forceinline__ void keep(bool there)  // zeros otherwise
+    {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i)
+            w[i] = there ? w[i] : 0u;
     }
     __device__ __forceinline__ void unpack(float (&x)[V]) const
     {
@@ -205,6 +217,13 @@ __device__ __forceinline__ int64_t uniform(int64_t x)
 {
     return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) |
            (int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
+}
+
+// A pointer to device memory that all lanes of the wavefront have, in scalar registers.
+template <typename T> __device__ __forceinline__ T *uniform_pointer(T *p)
+{
+    typedef __attribute__((address_space(1))) T *global;  // not a flat address
+    return (T *)(global)(uintptr_t)uniform((int64_t)(uintptr_t)p);
 }
 
 // A value that is formed here, not where it is used (the compiler would sink sums

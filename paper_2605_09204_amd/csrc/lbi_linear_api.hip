@@ -93,6 +93,15 @@ bool bad_attention_shape(int64_t T, int64_t sequences, int32_t H, int32_t KH, in
     return sequences == 0 ? T != 0 : !ragged && T % sequences != 0;
 }
 
+// The rows of a tile are addressed by 32-bit distances in bytes.
+bool too_wide(std::initializer_list<int64_t> strides)
+{
+    for (int64_t ld : strides)
+        if (ld > LBI_ATTENTION_MAX_LD)
+            return true;
+    return false;
+}
+
 lbi_status check_attention_inputs(const lbi_attention_inputs *in)
 {
     if (!in)
@@ -106,6 +115,8 @@ lbi_status check_attention_inputs(const lbi_attention_inputs *in)
         return LBI_ERR_NULL;
     if (in->T > 0 && (!in->q || !in->k || !in->v))
         return LBI_ERR_NULL;
+    if (too_wide({in->ld_q, in->ld_k, in->ld_v}))
+        return LBI_ERR_SHAPE;
     return LBI_OK;
 }
 
@@ -426,6 +437,8 @@ lbi_status lbi_linear_attention_backward(const lbi_attention_inputs *in, const v
     lbi_status st = check_attention_inputs(in);
     if (st != LBI_OK)
         return st;
+    if (too_wide({ld_dout}))
+        return LBI_ERR_SHAPE;
     if (!grads || (in->T > 0 && (!dout || !grads->dq || !grads->dk || !grads->dv)))
         return LBI_ERR_NULL;
     AttentionArgs a = {};

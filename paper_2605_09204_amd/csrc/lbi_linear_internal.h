@@ -93,7 +93,8 @@ struct AttentionArgs {
     int64_t ld_dout;
     const float *dstate_out;
     lbi_attention_gradients out;
-    float *marks;          // [ranges][H][attention_marks][DK][DV]: states on the way
+    float *marks;          // [ranges][H][attention_marks][DK][DV]: states on the way, less
+                           // what enters the range
     float *part_k, *part_v; // [T][H][DK or DV]: shared heads' gradients by head, KH < H only
     float *part_decay;     // [ranges][H]
 };
@@ -102,8 +103,10 @@ enum : int32_t { kPart = 1, kWhole = 2 };
 hipError_t launch_linear_attention(const AttentionArgs &a, hipStream_t stream);
 hipError_t launch_linear_attention_step(const AttentionArgs &a, hipStream_t stream);
 hipError_t launch_linear_attention_backward(const AttentionArgs &a, hipStream_t stream);
-// The forward's states at the ranges' ends, and (backward) the gradients at their starts.
-hipError_t launch_attention_ends(const AttentionArgs &a, bool backward, hipStream_t stream);
+// The states at the ranges' ends, or (backward) their gradients at the ranges' starts; with marks, the
+// states before tiles of tile_rows tokens, as far as the range they are in adds to them.
+hipError_t launch_attention_ends(const AttentionArgs &a, bool backward, int tile_rows, int marks,
+                                 hipStream_t stream);
 // States (or their gradients) of sequences without tokens.
 hipError_t launch_attention_empty(const AttentionArgs &a, bool backward, hipStream_t stream);
 

@@ -8,6 +8,7 @@
 // operands pass through LDS as they lie, and the matrix instructions' operands are read from there
 // straight or through the transposing read.
 #include "lbi_attention.hpp"
+#include "lbi_dma.hpp"
 
 namespace lbi {
 namespace {
@@ -126,6 +127,27 @@ __device__ __forceinline__ void finish(const ProductArgs &a, int64_t m, int n, c
     else finish_as<T, float, ACT>(a, m, n, v);
 }
 
+// A wavefront's results from row m0 and column n0 on, through the epilogue or into the partial sums.
+template <typename T, int MT, int NT, int ACT>
+__device__ __forceinline__ void finish_tile(const ProductArgs &a, const f4 (&acc)[MT][NT],
+                                            int64_t m0, int n0, int64_t split)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int64_t m = m0 + 16 * i + (lane & 15);
+            const int n = n0 + 16 * j + 4 * (lane >> 4);
+            if (m >= a.M || n >= a.N)
+                continue;
+            if (a.splits > 1)
+                store4(a.partial + (split * a.M + m) * a.N + n, a.N - n, acc[i][j]);
+            else
+                finish<T, ACT>(a, m, n, acc[i][j]);
+        }
+}
+
 template <typename T, bool A_COLS, bool B_COLS, int BM, int BN, int ACT>
 __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs a, int64_t first)
 {
@@ -134,7 +156,7 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs a, in
     using Sb = Staged<T, B_COLS, BN, BK>;
     __shared__ __align__(16) T tile_a[2][Sa::HEIGHT * Sa::STRIDE], tile_b[2][Sb::HEIGHT * Sb::STRIDE];
     constexpr int MT = BM / 32, NT = BN / 32;  // 16 x 16 results of a wavefront, a quarter of the tile
-    const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
+    const int wave = threadIdx.x >> 6;
     const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
     const int across = (a.N + BN - 1) / BN;
     uint32_t id = blockIdx.x;
@@ -184,19 +206,176 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs a, in
         }
         at ^= 1;
     }
+    finish_tile<T, MT, NT, ACT>(a, acc, m0 + wm, n0 + wn, rest % a.splits);
+}
+
+// ---- the product of operands that whole 16-byte pieces hold
+
+// A stage of an operand in LDS is SIZE rows (or columns) of 128 bytes of k: rows as lds_off lays
+// them, columns as [BK][SIZE] with the 16-value groups of a row exchanged, so that the rows that
+// a transposing read takes together (bf16: 4 of them and 4 eight rows on; float32: every fourth)
+// lie in different banks.
+template <typename T, int SIZE> struct Columns {
+    static constexpr int ROW = SIZE * (int)sizeof(T);  // bytes of a k
+    static __device__ __forceinline__ int group(int k)
+    {
+        if constexpr (sizeof(T) == 4)
+            return (k >> 2) & 3;
+        else if constexpr (SIZE == 128)
+            return (k & 3) | (k >> 1 & 4);
+        else
+            return (k >> 1 & 1) | (k >> 2 & 2);
+    }
+};
+template <typename T, bool COLS, int SIZE> struct DmaOperand {
+    static constexpr int BK = 128 / (int)sizeof(T), EACH = 16 / (int)sizeof(T);
+    static constexpr int LOADS = SIZE / 32;  // of 1 KB, by each of four wavefronts
+    const T *base;  // the first row, or column, at k = 0
+    int64_t ld;
+    int there;      // rows, or columns, that are there
+    int at[LOADS];  // this lane's bytes from the stage's first k
+    int piece[LOADS];  // its first k (rows) or column
+
+    __device__ __forceinline__ DmaOperand(const void *p, int64_t ld, int64_t first, int64_t count)
+        : ld(ld)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        base = (const T *)p + (COLS ? first : first * ld);
+        there = count - first < SIZE ? (int)(count - first) : SIZE;
+#pragma unroll
+        for (int d = 0; d < LOADS; ++d) {
+            const int byte = (wave + 4 * d) * 1024 + lane * 16;
+            if constexpr (COLS) {
+                using L = Columns<T, SIZE>;
+                const int k = byte / L::ROW, slot = byte % L::ROW / 16;
+                constexpr int PER = (int)sizeof(T);  // pieces of a group: 16 values
+                piece[d] = (slot ^ (L::group(k) * PER)) * EACH;
+                at[d] = k * (int)ld * (int)sizeof(T) + piece[d] * (int)sizeof(T);
+                if (piece[d] >= there)
+                    at[d] = kOutOfRange;
+            } else {
+                const int line = byte >> 8, slot = (byte >> 4 & 15) ^ (line & 7);
+                piece[d] = (slot & 7) * EACH;
+                at[d] = ((2 * line + (slot >> 3)) * (int)ld + piece[d]) * (int)sizeof(T);
+            }
+        }
+    }
+    // the stage from k on, of which `left` are there (left > 0)
+    __device__ __forceinline__ void issue(uint32_t lds, int64_t k, int64_t left) const
+    {
+        const int n = left < BK ? (int)left : BK;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        // the last row, or k, ends where its last piece does
+        const int64_t rows = COLS ? n : there, width = COLS ? there : n;
+        const i4 rs = dma_rsrc(base + (COLS ? k * ld : k),
+                               (uint32_t)(((rows - 1) * ld + width) * (int)sizeof(T)));
+#pragma unroll
+        for (int d = 0; d < LOADS; ++d) {
+            int v = at[d];
+            if constexpr (!COLS)
+                v = piece[d] < n ? v : kOutOfRange;
+            dma_b128(__builtin_amdgcn_readfirstlane(lds + (wave + 4 * d) * 1024), rs, v, 0);
+        }
+    }
+};
+typedef __attribute__((address_space(3))) char lds_char;
+
+// 32 values k from 32 kb on of the 16 rows, or columns, from 16 tile on, of a stage.
+template <typename T, bool COLS, int SIZE>
+__device__ __forceinline__ void stage_operand(Frag<T> &f, uint32_t stage, int tile, int kb)
+{
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    if constexpr (!COLS) {
+        if constexpr (sizeof(T) == 2) {
+            f.w = *(const u4 *)(lds_char *)(uintptr_t)(stage + tile * 2048 + lds_off(c, 4 * kb + g) * 2);
+        } else {
+            const f4 a = *(const f4 *)(lds_char *)(uintptr_t)(stage + tile * 2048 + lds_off(c, g) * 2);
+            const f4 b = *(const f4 *)(lds_char *)(uintptr_t)(stage + tile * 2048 + lds_off(c, 4 + g) * 2);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                f.v[r] = a[r];
+                f.v[4 + r] = b[r];
+            }
+        }
+    } else {
+        using L = Columns<T, SIZE>;
+        if constexpr (sizeof(T) == 2) {
+            const int k = 32 * kb + 8 * g + (c >> 2);
+            const uint32_t p = stage + k * L::ROW + (tile ^ L::group(k)) * 32 + (c & 3) * 8;
+            typedef __attribute__((address_space(3))) s4 lds_s4;
+            const u2 a = __builtin_bit_cast(
+                u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(uintptr_t)p));
+            const u2 b = __builtin_bit_cast(
+                u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(uintptr_t)(p + 4 * L::ROW)));
+            f.w = u4{a.x, a.y, b.x, b.y};
+        } else {
+            const uint32_t p = stage + 4 * g * L::ROW + (tile ^ L::group(4 * g)) * 64 + c * 4;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                f.v[r] = *(const float *)(lds_char *)(uintptr_t)(p + r * L::ROW);
+                f.v[4 + r] = *(const float *)(lds_char *)(uintptr_t)(p + (16 + r) * L::ROW);
+            }
+        }
+    }
+}
+
+template <typename T, bool A_COLS, bool B_COLS, int BM, int BN, int ACT>
+__global__ __launch_bounds__(256, 2) void product_dma_kernel(const ProductArgs a, int64_t first)
+{
+    constexpr int BK = 128 / (int)sizeof(T), A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
+    __shared__ __align__(1024) char smem[2 * STAGE];
+    const uint32_t lds = (uint32_t)(uintptr_t)(lds_char *)smem;
+    constexpr int MT = BM / 32, NT = BN / 32;  // 16 x 16 results of a wavefront, a quarter of the tile
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = (wave >> 1) * MT, wn = (wave & 1) * NT;
+    const int across = (a.N + BN - 1) / BN;
+    uint32_t id = blockIdx.x;
+    if (gridDim.x % 8 == 0)
+        id = id % 8 * (gridDim.x / 8) + id / 8;
+    const int n0 = (int)(id % across) * BN;
+    const int64_t rest = first + id / across;
+    const int64_t m0 = rest / a.splits * BM;
+    const int64_t k_first = rest % a.splits * a.split;
+    const int64_t k_end = k_first + a.split < a.K ? k_first + a.split : a.K;
+    const DmaOperand<T, A_COLS, BM> pa(a.a, a.ld_a, m0, a.M);
+    const DmaOperand<T, B_COLS, BN> pb(a.b, a.ld_b, n0, a.N);
+    f4 acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const int64_t m = m0 + wm + 16 * i + c16;
-            const int n = n0 + wn + 16 * j + 4 * g;
-            if (m >= a.M || n >= a.N)
-                continue;
-            if (a.splits > 1)
-                store4(a.partial + ((rest % a.splits) * a.M + m) * a.N + n, a.N - n, acc[i][j]);
-            else
-                finish<T, ACT>(a, m, n, acc[i][j]);
+        for (int j = 0; j < NT; ++j)
+            acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    auto issue = [&](int64_t k, uint32_t stage) {
+        pa.issue(stage, k, k_end - k);
+        pb.issue(stage + A_BYTES, k, k_end - k);
+    };
+    if (k_first < k_end)
+        issue(k_first, lds);
+    uint32_t at = 0;
+    for (int64_t k = k_first; k < k_end; k += BK) {
+        phase();
+        dma_barrier<0>();  // this stage is there, and the one before it has been read
+        phase();
+        if (k + BK < k_end)
+            issue(k + BK, lds + (STAGE - at));
+#pragma unroll
+        for (int kb = 0; kb < BK / 32; ++kb) {
+            Frag<T> fa[MT], fb[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                stage_operand<T, B_COLS, BN>(fb[j], lds + at + A_BYTES, wn + j, kb);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                stage_operand<T, A_COLS, BM>(fa[i], lds + at, wm + i, kb);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+                    mma(acc[i][j], fb[j], fa[i]);
         }
+        at = STAGE - at;
+    }
+    finish_tile<T, MT, NT, ACT>(a, acc, m0 + 16 * wm, n0 + 16 * wn, rest % a.splits);
 }
 
 // The sum of the splits' partial results, in order, through the epilogue.
@@ -281,12 +460,27 @@ int tile_of(const ProductArgs &a)
     return big >= 256 || a.K >= 4096 ? 128 : 64;
 }
 
+// Whether the operands may be loaded straight into LDS: 16-byte pieces of rows that begin and end
+// with them, at distances that a buffer's 32 bits hold.
+bool in_pieces(const ProductArgs &a)
+{
+    const int64_t each = a.bf16 ? 8 : 4;
+    auto fits = [&](const void *p, int64_t ld, int64_t width) {
+        return ((uintptr_t)p & 15) == 0 && ld % each == 0 && width % each == 0 && ld <= 1 << 20;
+    };
+    return fits(a.a, a.ld_a, a.a_cols ? a.M : a.K) && fits(a.b, a.ld_b, a.b_cols ? a.N : a.K);
+}
+
 template <typename T, bool A_COLS, bool B_COLS, int TILE, int ACT>
 hipError_t product(const ProductArgs &a, hipStream_t stream)
 {
     const int64_t across = (a.N + TILE - 1) / TILE, down = (a.M + TILE - 1) / TILE;
+    const bool pieces = in_pieces(a);
     return in_launches(down * a.splits, across, [&](int64_t first, dim3 grid) {
-        product_kernel<T, A_COLS, B_COLS, TILE, TILE, ACT><<<grid, 256, 0, stream>>>(a, first);
+        if (pieces)
+            product_dma_kernel<T, A_COLS, B_COLS, TILE, TILE, ACT><<<grid, 256, 0, stream>>>(a, first);
+        else
+            product_kernel<T, A_COLS, B_COLS, TILE, TILE, ACT><<<grid, 256, 0, stream>>>(a, first);
     });
 }
 template <typename T> hipError_t product_by(const ProductArgs &a, hipStream_t stream)

@@ -47,6 +47,7 @@
 #include <type_traits>
 
 #include "lbi_device.hpp"
+#include "lbi_dma.hpp"
 #include "lbi_internal.h"
 #include "lbi_region_args.hpp"
 
@@ -94,16 +95,6 @@ __device__ __forceinline__ float wave_sum(float x)
 }
 
 // ---- the tile pipeline shared by both products ---------------------------------
-// LDS tile layout: 128 rows of 64 bf16 (eight 16-byte chunks), two rows per
-// 256-byte line, chunk q of row R at line R / 2, slot ((R & 1) 8 + q) ^ (R / 2 & 7).
-// The 16 lanes that a b128 access serves together then touch 16 distinct
-// slots (all 64 banks) both when they read one chunk of 16 consecutive rows
-// (an MFMA operand) and when they write the 8 chunks of 2 consecutive rows.
-__device__ __forceinline__ int lds_off(int row, int q)
-{
-    return (row >> 1) * 128 + ((((row & 1) << 3) + q) ^ ((row >> 1) & 7)) * 8;
-}
-
 // 128 rows x 64 k of a row-major bf16 matrix (row stride ld) from row0, k0;
 // rows >= nrows read as zero.  Thread t loads chunks c = t + 256 i: row c / 8,
 // chunk c % 8, at the per-lane byte offsets voff (tile_offsets).  One buffer
@@ -142,41 +133,7 @@ __device__ __forceinline__ void tile_store(const u4 (&v)[4], __bf16 *s)
     }
 }
 
-// ---- operands loaded straight into LDS ---------------------------------------------
-typedef int i4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ i4 dma_rsrc(const void *base, uint32_t bytes)
-{
-    // (the values are wave-uniform; the scalar registers an asm operand of
-    // class "s" needs are made explicit)
-    const uint64_t x = (uint64_t)(uintptr_t)base;
-    i4 v;
-    v[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)x);
-    v[1] = __builtin_amdgcn_readfirstlane((int)((uint32_t)(x >> 32) & 0xFFFFu));
-    v[2] = __builtin_amdgcn_readfirstlane((int)bytes);
-    v[3] = kBufferWord3;
-    return v;
-}
-// 16 bytes per lane from rs at voff + soff into LDS at lds + 16 lane; M0 (the
-// LDS destination, one wait state after writing it) is saved and restored in
-// the asm
-__device__ __forceinline__ void dma_b128(uint32_t lds, i4 rs, int voff, int soff)
-{
-    uint32_t keep;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
-                 "buffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep)
-                 : "s"(lds), "v"(voff), "s"(rs), "s"(soff)
-                 : "memory");
-}
-// all of this wave's loads but the N most recent, and its LDS operations, done;
-// then the workgroup barrier (the waits are the compiler's own, so it counts
-// them when it places its LDS waits)
-template <int N> __device__ __forceinline__ void dma_barrier()
-{
-    __builtin_amdgcn_s_waitcnt((N & 15) | (((N >> 4) & 3) << 14) | (7 << 4));
-    __builtin_amdgcn_s_barrier();
-}
-
+// ---- operands loaded straight into LDS (lbi_dma.hpp) -------------------------------
 // this wave's loads done, and no memory operation moved over the wait
 __device__ __forceinline__ void dma_wait()
 {
