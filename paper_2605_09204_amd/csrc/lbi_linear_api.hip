@@ -374,7 +374,7 @@ size_t lbi_linear_attention_workspace_bytes(int64_t T, int64_t sequences, int32_
         return 0;
     AttentionArgs a = {};
     a.in = attention_sizes(T, sequences, H, KH, DK, DV, dt);
-    a.cut = attention_cut(a.in, ragged != 0);
+    a.cut = attention_cut(a.in, ragged != 0, false);
     return attention_layout(a, nullptr);
 }
 
@@ -396,7 +396,7 @@ lbi_status lbi_linear_attention(const lbi_attention_inputs *in, void *o, int64_t
     a.o = o; a.ld_o = ld_o;
     a.state_out = state_out;
     a.slots = slots; a.n_slots = n_slots;
-    a.cut = attention_cut(*in, in->offsets != nullptr);
+    a.cut = attention_cut(*in, in->offsets != nullptr, false);
     const size_t need = attention_layout(a, workspace);
     if (!in->state_in || in->state_in != state_out)
         a.starts = nullptr;  // nothing writes what begins
@@ -425,7 +425,7 @@ size_t lbi_linear_attention_backward_workspace_bytes(int64_t T, int64_t sequence
         return 0;
     AttentionArgs a = {};
     a.in = attention_sizes(T, sequences, H, KH, DK, DV, dt);
-    a.cut = attention_cut(a.in, ragged != 0);
+    a.cut = attention_cut(a.in, ragged != 0, true);
     return attention_backward_layout(a, nullptr);
 }
 
@@ -446,7 +446,7 @@ lbi_status lbi_linear_attention_backward(const lbi_attention_inputs *in, const v
     a.dout = dout; a.ld_dout = ld_dout;
     a.dstate_out = dstate_out;
     a.out = *grads;
-    a.cut = attention_cut(*in, in->offsets != nullptr);
+    a.cut = attention_cut(*in, in->offsets != nullptr, true);
     const size_t need = attention_backward_layout(a, workspace);
     st = check_workspace(workspace, workspace_bytes, need);
     if (st != LBI_OK)

@@ -67,7 +67,7 @@ struct AttentionCut {
     int32_t per_sequence;
     bool joined;  // states pass between ranges
 };
-AttentionCut attention_cut(const lbi_attention_inputs &in, bool ragged);
+AttentionCut attention_cut(const lbi_attention_inputs &in, bool ragged, bool backward);
 constexpr int kAttentionTile = 64;  // the unit of a cut's tokens
 // States that the gradient keeps of a range and head, one of them for scratch.
 int64_t attention_marks(const lbi_attention_inputs &in, const AttentionCut &cut);

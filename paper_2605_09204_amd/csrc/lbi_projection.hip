@@ -58,6 +58,42 @@ __device__ __forceinline__ void operand(Frag<T> &f, const T *m, int stride, int 
     }
 }
 
+// What the matrix cores are given of an operand.  Float32 values go in as three bf16 values that
+// add up to them: of the nine products of two such sums the six down to 2^-16 of the first are
+// taken, which leaves what float32 products round away (the library's default arithmetic for
+// float32), at 6 / 16 of the float32 matrix cores' time.
+template <typename T> struct Factor;
+template <> struct Factor<bf16_bits> {
+    Frag<bf16_bits> f;
+    __device__ __forceinline__ void set(const Frag<bf16_bits> &x) { f = x; }
+};
+template <> struct Factor<float> {
+    Frag<bf16_bits> h, m, l;
+    __device__ __forceinline__ void set(const Frag<float> &x)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const Split2 s = split_pair(x.v[2 * i], x.v[2 * i + 1]);
+            h.w[i] = s.h;
+            m.w[i] = s.m;
+            l.w[i] = s.l;
+        }
+    }
+};
+__device__ __forceinline__ void mma(f4 &acc, const Factor<bf16_bits> &a, const Factor<bf16_bits> &b)
+{
+    mma(acc, a.f, b.f);
+}
+__device__ __forceinline__ void mma(f4 &acc, const Factor<float> &a, const Factor<float> &b)
+{
+    mma(acc, a.m, b.m);
+    mma(acc, a.h, b.l);
+    mma(acc, a.l, b.h);
+    mma(acc, a.h, b.m);
+    mma(acc, a.m, b.h);
+    mma(acc, a.h, b.h);
+}
+
 // A tile of an operand: [SIZE][BK] of rows or [BK][SIZE], in registers on its way to LDS.
 template <typename T, bool COLS, int SIZE, int BK> struct Staged {
     static constexpr int WIDTH = COLS ? SIZE : BK, HEIGHT = COLS ? BK : SIZE;
@@ -191,14 +227,18 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs a, in
             load(k + BK);
 #pragma unroll
         for (int kb = 0; kb < BK; kb += 32) {
-            Frag<T> fb[NT];
+            Factor<T> fb[NT];
+            Frag<T> f;
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-                operand<T, B_COLS>(fb[j], tile_b[at], Sb::STRIDE, wn + 16 * j, kb);
+            for (int j = 0; j < NT; ++j) {
+                operand<T, B_COLS>(f, tile_b[at], Sb::STRIDE, wn + 16 * j, kb);
+                fb[j].set(f);
+            }
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                Frag<T> fa;
-                operand<T, A_COLS>(fa, tile_a[at], Sa::STRIDE, wm + 16 * i, kb);
+                Factor<T> fa;
+                operand<T, A_COLS>(f, tile_a[at], Sa::STRIDE, wm + 16 * i, kb);
+                fa.set(f);
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
                     mma(acc[i][j], fb[j], fa);
@@ -360,18 +400,25 @@ __global__ __launch_bounds__(256, 2) void product_dma_kernel(const ProductArgs a
             issue(k + BK, lds + (STAGE - at));
 #pragma unroll
         for (int kb = 0; kb < BK / 32; ++kb) {
-            Frag<T> fa[MT], fb[NT];
+            Frag<T> xa[MT], xb[NT];
 #pragma unroll
             for (int j = 0; j < NT; ++j)
-                stage_operand<T, B_COLS, BN>(fb[j], lds + at + A_BYTES, wn + j, kb);
+                stage_operand<T, B_COLS, BN>(xb[j], lds + at + A_BYTES, wn + j, kb);
 #pragma unroll
             for (int i = 0; i < MT; ++i)
-                stage_operand<T, A_COLS, BM>(fa[i], lds + at, wm + i, kb);
+                stage_operand<T, A_COLS, BM>(xa[i], lds + at, wm + i, kb);
+            Factor<T> fb[NT];
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int j = 0; j < NT; ++j)
+                fb[j].set(xb[j]);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                Factor<T> fa;
+                fa.set(xa[i]);
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
-                    mma(acc[i][j], fb[j], fa[i]);
+                    mma(acc[i][j], fb[j], fa);
+            }
         }
         at = STAGE - at;
     }
