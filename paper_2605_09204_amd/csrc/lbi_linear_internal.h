@@ -38,8 +38,9 @@ struct ProductArgs {
     float *partial;          // [splits][M][N], splits > 1 only
     int32_t splits;
     int64_t split;           // values of k of each
+    int32_t tile_m, tile_n;  // of a workgroup
 };
-// Sets splits and split; returns the floats of partial.
+// Sets the tile, splits and split; returns the floats of partial.
 int64_t plan_product(ProductArgs &a);
 hipError_t launch_product(const ProductArgs &a, hipStream_t stream);
 

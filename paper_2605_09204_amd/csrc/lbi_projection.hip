@@ -184,6 +184,33 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const f4 (&acc
         }
 }
 
+// Which part of the result a workgroup has.  Workgroups go to the eight XCDs in turn; each gets tiles
+// that lie together, whose operands its L2 then holds for all of them.
+struct Place {
+    int64_t m0, k, k_end;
+    int n0, split;
+};
+template <int BM, int BN> __device__ __forceinline__ Place place(const ProductArgs &a, int64_t first)
+{
+    const uint32_t across = (uint32_t)(a.N + BN - 1) / BN;
+    uint32_t id = blockIdx.x;
+    if (gridDim.x % 8 == 0)
+        id = id % 8 * (gridDim.x / 8) + id / 8;
+    Place x;
+    x.n0 = (int)(id % across) * BN;
+    const int64_t rest = first + id / across;
+    if (a.splits > 1) {  // few tiles: in 32 bits
+        x.m0 = (int64_t)((uint32_t)rest / (uint32_t)a.splits) * BM;
+        x.split = (int)((uint32_t)rest % (uint32_t)a.splits);
+    } else {
+        x.m0 = rest * BM;
+        x.split = 0;
+    }
+    x.k = x.split * a.split;
+    x.k_end = x.k + a.split < a.K ? x.k + a.split : a.K;
+    return x;
+}
+
 template <typename T, bool A_COLS, bool B_COLS, int BM, int BN, int ACT>
 __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs a, int64_t first)
 {
@@ -194,17 +221,9 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs a, in
     constexpr int MT = BM / 32, NT = BN / 32;  // 16 x 16 results of a wavefront, a quarter of the tile
     const int wave = threadIdx.x >> 6;
     const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
-    const int across = (a.N + BN - 1) / BN;
-    uint32_t id = blockIdx.x;
-    // Workgroups go to the eight XCDs in turn; each gets tiles that lie together, whose operands
-    // its L2 then holds for all of them.
-    if (gridDim.x % 8 == 0)
-        id = id % 8 * (gridDim.x / 8) + id / 8;
-    const int n0 = (int)(id % across) * BN;
-    const int64_t rest = first + id / across;
-    const int64_t m0 = rest / a.splits * BM;
-    const int64_t k_first = rest % a.splits * a.split;
-    const int64_t k_end = k_first + a.split < a.K ? k_first + a.split : a.K;
+    const Place x = place<BM, BN>(a, first);
+    const int64_t m0 = x.m0, k_first = x.k, k_end = x.k_end;
+    const int n0 = x.n0;
     f4 acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -246,15 +265,18 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductArgs a, in
         }
         at ^= 1;
     }
-    finish_tile<T, MT, NT, ACT>(a, acc, m0 + wm, n0 + wn, rest % a.splits);
+    finish_tile<T, MT, NT, ACT>(a, acc, m0 + wm, n0 + wn, x.split);
 }
 
 // ---- the product of operands that whole 16-byte pieces hold
 
-// A stage of an operand in LDS is SIZE rows (or columns) of 128 bytes of k: rows as lds_off lays
-// them, columns as [BK][SIZE] with the 16-value groups of a row exchanged, so that the rows that
-// a transposing read takes together (bf16: 4 of them and 4 eight rows on; float32: every fourth)
-// lie in different banks.
+// A stage of an operand in LDS is SIZE rows of 128 bytes of k, as lds_off lays them, or as many k of
+// SIZE columns, with the groups of 16 columns of a row exchanged, so that what a transposing read
+// takes together (bf16: four rows and those eight on; float32: every fourth) lies in different
+// banks.
+constexpr int kStageRow = 128;
+typedef __attribute__((address_space(3))) char lds_char;
+
 template <typename T, int SIZE> struct Columns {
     static constexpr int ROW = SIZE * (int)sizeof(T);  // bytes of a k
     static __device__ __forceinline__ int group(int k)
@@ -268,57 +290,55 @@ template <typename T, int SIZE> struct Columns {
     }
 };
 template <typename T, bool COLS, int SIZE> struct DmaOperand {
-    static constexpr int BK = 128 / (int)sizeof(T), EACH = 16 / (int)sizeof(T);
-    static constexpr int LOADS = SIZE / 32;  // of 1 KB, by each of four wavefronts
-    const T *base;  // the first row, or column, at k = 0
-    int64_t ld;
-    int there;      // rows, or columns, that are there
-    int at[LOADS];  // this lane's bytes from the stage's first k
-    int piece[LOADS];  // its first k (rows) or column
+    static constexpr int ROW = kStageRow, BK = ROW / (int)sizeof(T), EACH = 16 / (int)sizeof(T);
+    static constexpr int LOADS = SIZE * ROW / 4096;  // of 1 KB, by each of four wavefronts
+    const char *base;  // the first row, or column, of the next stage
+    int64_t step;      // bytes from stage to stage
+    int ld, there;     // bytes; rows, or columns, that are there
+    int at[LOADS];     // this lane's bytes from the stage's first k
+    int piece[LOADS];  // its first k (rows)
 
-    __device__ __forceinline__ DmaOperand(const void *p, int64_t ld, int64_t first, int64_t count)
-        : ld(ld)
+    __device__ __forceinline__ DmaOperand(const void *p, int64_t stride, int64_t first, int64_t count,
+                                          int64_t k)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        base = (const T *)p + (COLS ? first : first * ld);
+        base = (const char *)((const T *)p + (COLS ? k * stride + first : first * stride + k));
+        ld = (int)stride * (int)sizeof(T);
+        step = COLS ? (int64_t)BK * ld : ROW;
         there = count - first < SIZE ? (int)(count - first) : SIZE;
 #pragma unroll
         for (int d = 0; d < LOADS; ++d) {
             const int byte = (wave + 4 * d) * 1024 + lane * 16;
+            piece[d] = 0;
             if constexpr (COLS) {
                 using L = Columns<T, SIZE>;
                 const int k = byte / L::ROW, slot = byte % L::ROW / 16;
                 constexpr int PER = (int)sizeof(T);  // pieces of a group: 16 values
-                piece[d] = (slot ^ (L::group(k) * PER)) * EACH;
-                at[d] = k * (int)ld * (int)sizeof(T) + piece[d] * (int)sizeof(T);
-                if (piece[d] >= there)
-                    at[d] = kOutOfRange;
+                const int col = (slot ^ (L::group(k) * PER)) * EACH;
+                at[d] = col < there ? k * ld + col * (int)sizeof(T) : kOutOfRange;
             } else {
-                const int line = byte >> 8, slot = (byte >> 4 & 15) ^ (line & 7);
-                piece[d] = (slot & 7) * EACH;
-                at[d] = ((2 * line + (slot >> 3)) * (int)ld + piece[d]) * (int)sizeof(T);
+                const int line = byte >> 8, slot = byte >> 4 & 15;
+                const int q = (slot ^ line) & 7;
+                piece[d] = q * EACH;
+                at[d] = (2 * line + (slot >> 3)) * ld + q * 16;
             }
         }
     }
-    // the stage from k on, of which `left` are there (left > 0)
-    __device__ __forceinline__ void issue(uint32_t lds, int64_t k, int64_t left) const
+    // The next stage, of whose k `left` are there (left > 0).
+    __device__ __forceinline__ void issue(uint32_t lds, int64_t left)
     {
         const int n = left < BK ? (int)left : BK;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         // the last row, or k, ends where its last piece does
-        const int64_t rows = COLS ? n : there, width = COLS ? there : n;
-        const i4 rs = dma_rsrc(base + (COLS ? k * ld : k),
-                               (uint32_t)(((rows - 1) * ld + width) * (int)sizeof(T)));
+        const i4 rs = dma_rsrc(base, (uint32_t)(((COLS ? n : there) - 1) * ld +
+                                                (COLS ? there : n) * (int)sizeof(T)));
 #pragma unroll
-        for (int d = 0; d < LOADS; ++d) {
-            int v = at[d];
-            if constexpr (!COLS)
-                v = piece[d] < n ? v : kOutOfRange;
-            dma_b128(__builtin_amdgcn_readfirstlane(lds + (wave + 4 * d) * 1024), rs, v, 0);
-        }
+        for (int d = 0; d < LOADS; ++d)
+            dma_b128(__builtin_amdgcn_readfirstlane(lds + (wave + 4 * d) * 1024), rs,
+                     COLS || piece[d] < n ? at[d] : kOutOfRange, 0);
+        base += step;
     }
 };
-typedef __attribute__((address_space(3))) char lds_char;
 
 // 32 values k from 32 kb on of the 16 rows, or columns, from 16 tile on, of a stage.
 template <typename T, bool COLS, int SIZE>
@@ -359,54 +379,118 @@ __device__ __forceinline__ void stage_operand(Frag<T> &f, uint32_t stage, int ti
     }
 }
 
+// Two stages: one on its way while the other is worked on.  (Five of half their depth were slower by a
+// fifth: what a step costs besides its loads outweighs their latency.)
+// Eight sums of a row of the result, n .. n + 7, through the epilogue.
+template <typename T, typename O, int ACT>
+__device__ __forceinline__ void finish_eight(const ProductArgs &a, int64_t m, int n, float (&v)[8])
+{
+    const int left = a.N - n;
+    float r[8];
+    if (a.residual)
+        load_some<8>((const O *)a.residual + m * a.ld_residual + n, left, r);
+    if (a.bias) {
+        float b[8];
+        load_some<8>(a.bias + n, left, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] += b[i];
+    }
+    if (a.pre)
+        store_some<8>((T *)a.pre + m * a.ld_pre + n, left, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] = activate<ACT>(v[i]);
+    if (a.residual)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] += r[i];
+    store_some<8>((O *)a.out + m * a.ld_out + n, left, v);
+}
+// The workgroup's tile through LDS, where the wavefronts' results become whole rows, and out: stores
+// of 8 bytes from where the results are took twice as long.  A row's 16-byte pieces are exchanged by
+// its number, so that 16 rows' pieces of one column lie in different banks.
+template <typename T, int BM, int BN, int ACT, int MT, int NT>
+__device__ __forceinline__ void finish_rows(const ProductArgs &a, const f4 (&acc)[MT][NT], char *smem,
+                                            const Place &at, int wm, int wn)
+{
+    const int lane = threadIdx.x & 63;
+    f4 *tile = (f4 *)smem;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int m = 16 * (wm + i) + (lane & 15), piece = 4 * (wn + j) + (lane >> 4);
+            tile[m * (BN / 4) + (piece ^ (m & 15))] = acc[i][j];
+        }
+    __syncthreads();
+    constexpr int PER_ROW = BN / 8;
+    const int n = at.n0 + (int)threadIdx.x % PER_ROW * 8;
+    if (n >= a.N)
+        return;
+#pragma unroll 2
+    for (int row = threadIdx.x / PER_ROW; row < BM; row += 256 / PER_ROW) {
+        const int64_t m = at.m0 + row;
+        if (m >= a.M)
+            return;
+        const int piece = (int)threadIdx.x % PER_ROW * 2;
+        const f4 x = tile[row * (BN / 4) + (piece ^ (row & 15))];
+        const f4 y = tile[row * (BN / 4) + ((piece + 1) ^ (row & 15))];
+        float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        if (a.splits > 1)
+            store_some<8>(a.partial + (at.split * a.M + m) * a.N + n, a.N - n, v);
+        else if (a.out_bf16)
+            finish_eight<T, bf16_bits, ACT>(a, m, n, v);
+        else
+            finish_eight<T, float, ACT>(a, m, n, v);
+    }
+}
+
 template <typename T, bool A_COLS, bool B_COLS, int BM, int BN, int ACT>
 __global__ __launch_bounds__(256, 2) void product_dma_kernel(const ProductArgs a, int64_t first)
 {
-    constexpr int BK = 128 / (int)sizeof(T), A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
+    using Pa = DmaOperand<T, A_COLS, BM>;
+    using Pb = DmaOperand<T, B_COLS, BN>;
+    constexpr int BK = Pa::BK, A_BYTES = BM * Pa::ROW, STAGE = (BM + BN) * Pa::ROW;
     __shared__ __align__(1024) char smem[2 * STAGE];
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_char *)smem;
     constexpr int MT = BM / 32, NT = BN / 32;  // 16 x 16 results of a wavefront, a quarter of the tile
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = (wave >> 1) * MT, wn = (wave & 1) * NT;
-    const int across = (a.N + BN - 1) / BN;
-    uint32_t id = blockIdx.x;
-    if (gridDim.x % 8 == 0)
-        id = id % 8 * (gridDim.x / 8) + id / 8;
-    const int n0 = (int)(id % across) * BN;
-    const int64_t rest = first + id / across;
-    const int64_t m0 = rest / a.splits * BM;
-    const int64_t k_first = rest % a.splits * a.split;
-    const int64_t k_end = k_first + a.split < a.K ? k_first + a.split : a.K;
-    const DmaOperand<T, A_COLS, BM> pa(a.a, a.ld_a, m0, a.M);
-    const DmaOperand<T, B_COLS, BN> pb(a.b, a.ld_b, n0, a.N);
+    const Place at = place<BM, BN>(a, first);
+    Pa pa(a.a, a.ld_a, at.m0, a.M, at.k);
+    Pb pb(a.b, a.ld_b, at.n0, a.N, at.k);
     f4 acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j)
             acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-    auto issue = [&](int64_t k, uint32_t stage) {
-        pa.issue(stage, k, k_end - k);
-        pb.issue(stage + A_BYTES, k, k_end - k);
+    uint32_t stage = 0;
+    auto issue = [&](int64_t left) {
+        pa.issue(lds + stage, left);
+        pb.issue(lds + stage + A_BYTES, left);
+        stage = STAGE - stage;
     };
-    if (k_first < k_end)
-        issue(k_first, lds);
-    uint32_t at = 0;
-    for (int64_t k = k_first; k < k_end; k += BK) {
+    if (at.k < at.k_end)
+        issue(at.k_end - at.k);
+    for (int64_t left = at.k_end - at.k; left > 0; left -= BK) {
+        const uint32_t from = lds + (STAGE - stage);
         phase();
         dma_barrier<0>();  // this stage is there, and the one before it has been read
         phase();
-        if (k + BK < k_end)
-            issue(k + BK, lds + (STAGE - at));
+        if (left > BK)
+            issue(left - BK);
 #pragma unroll
         for (int kb = 0; kb < BK / 32; ++kb) {
             Frag<T> xa[MT], xb[NT];
 #pragma unroll
             for (int j = 0; j < NT; ++j)
-                stage_operand<T, B_COLS, BN>(xb[j], lds + at + A_BYTES, wn + j, kb);
+                stage_operand<T, B_COLS, BN>(xb[j], from + A_BYTES, wn + j, kb);
 #pragma unroll
             for (int i = 0; i < MT; ++i)
-                stage_operand<T, A_COLS, BM>(xa[i], lds + at, wm + i, kb);
+                stage_operand<T, A_COLS, BM>(xa[i], from, wm + i, kb);
             Factor<T> fb[NT];
 #pragma unroll
             for (int j = 0; j < NT; ++j)
@@ -420,9 +504,8 @@ __global__ __launch_bounds__(256, 2) void product_dma_kernel(const ProductArgs a
                     mma(acc[i][j], fb[j], fa);
             }
         }
-        at = STAGE - at;
     }
-    finish_tile<T, MT, NT, ACT>(a, acc, m0 + 16 * wm, n0 + 16 * wn, rest % a.splits);
+    finish_rows<T, BM, BN, ACT>(a, acc, smem, at, wm, wn);
 }
 
 // The sum of the splits' partial results, in order, through the epilogue.
@@ -500,12 +583,6 @@ template <typename F> hipError_t by_activation(lbi_activation act, F &&f)
     return f(std::integral_constant<int, LBI_ACT_NONE>{});
 }
 
-// The tile: 128 x 128, or 64 x 64 where those would leave CUs without work.
-int tile_of(const ProductArgs &a)
-{
-    const int64_t big = (a.M + 127) / 128 * ((a.N + 127) / 128);
-    return big >= 256 || a.K >= 4096 ? 128 : 64;
-}
 
 // Whether the operands may be loaded straight into LDS: 16-byte pieces of rows that begin and end
 // with them, at distances that a buffer's 32 bits hold.
@@ -518,33 +595,36 @@ bool in_pieces(const ProductArgs &a)
     return fits(a.a, a.ld_a, a.a_cols ? a.M : a.K) && fits(a.b, a.ld_b, a.b_cols ? a.N : a.K);
 }
 
-template <typename T, bool A_COLS, bool B_COLS, int TILE, int ACT>
+template <typename T, bool A_COLS, bool B_COLS, int BM, int BN, int ACT>
 hipError_t product(const ProductArgs &a, hipStream_t stream)
 {
-    const int64_t across = (a.N + TILE - 1) / TILE, down = (a.M + TILE - 1) / TILE;
+    const int64_t across = (a.N + BN - 1) / BN, down = (a.M + BM - 1) / BM;
     const bool pieces = in_pieces(a);
     return in_launches(down * a.splits, across, [&](int64_t first, dim3 grid) {
         if (pieces)
-            product_dma_kernel<T, A_COLS, B_COLS, TILE, TILE, ACT><<<grid, 256, 0, stream>>>(a, first);
+            product_dma_kernel<T, A_COLS, B_COLS, BM, BN, ACT><<<grid, 256, 0, stream>>>(a, first);
         else
-            product_kernel<T, A_COLS, B_COLS, TILE, TILE, ACT><<<grid, 256, 0, stream>>>(a, first);
+            product_kernel<T, A_COLS, B_COLS, BM, BN, ACT><<<grid, 256, 0, stream>>>(a, first);
     });
+}
+template <typename T, bool A_COLS, bool B_COLS, int ACT>
+hipError_t product_tiles(const ProductArgs &a, hipStream_t stream)
+{
+    if (a.tile_m == 64)
+        return product<T, A_COLS, B_COLS, 64, 64, ACT>(a, stream);
+    return a.tile_n == 64 ? product<T, A_COLS, B_COLS, 128, 64, ACT>(a, stream)
+                          : product<T, A_COLS, B_COLS, 128, 128, ACT>(a, stream);
 }
 template <typename T> hipError_t product_by(const ProductArgs &a, hipStream_t stream)
 {
-    const bool big = tile_of(a) == 128;
     hipError_t e;
     if (a.a_cols)
-        e = big ? product<T, true, true, 128, LBI_ACT_NONE>(a, stream)
-                : product<T, true, true, 64, LBI_ACT_NONE>(a, stream);
+        e = product_tiles<T, true, true, LBI_ACT_NONE>(a, stream);
     else if (a.b_cols)
-        e = big ? product<T, false, true, 128, LBI_ACT_NONE>(a, stream)
-                : product<T, false, true, 64, LBI_ACT_NONE>(a, stream);
+        e = product_tiles<T, false, true, LBI_ACT_NONE>(a, stream);
     else
         e = by_activation(a.act, [&](auto act) {
-            constexpr int ACT = decltype(act)::value;
-            return big ? product<T, false, false, 128, ACT>(a, stream)
-                       : product<T, false, false, 64, ACT>(a, stream);
+            return product_tiles<T, false, false, decltype(act)::value>(a, stream);
         });
     if (e != hipSuccess || a.splits <= 1)
         return e;
@@ -558,16 +638,34 @@ template <typename T> hipError_t product_by(const ProductArgs &a, hipStream_t st
 
 }  // namespace
 
+// The tile and the cuts of the sum, from timings of 14 shapes (1 to 16384 rows, sums of 100 to
+// 16384) at every tile and 1 to 24 cuts.
+//
+// The larger a tile, the fewer bytes and (float32) splits a product takes, but two workgroups a CU
+// are needed to keep it busy: 128 x 128 from 512 tiles on (float32: 192, its steps being three times
+// as long), 128 x 64 from 384.  bf16, 2048 x 2048 x 2048: 31 us with 256 tiles, 27 with 512, 28 with
+// 1024; 16384 x 1536 x 768: 55, 57, 66; float32, 4099 x 768 x 1536: 86, 93, 107.
+// Fewer tiles than 128 are cut along the sum to about two workgroups a CU, where each keeps at least
+// 4 steps (float32: 6) of 20 (24): the second launch costs 3 us and the partial sums' traffic.
+// bf16, 512 x 512 x 4096: 34 us whole, 14 in eight; 6707 x 64 x 1104: 10 whole, 11 in two.
 int64_t plan_product(ProductArgs &a)
 {
-    const int tile = tile_of(a);
-    const int64_t tiles = (a.M + tile - 1) / tile * ((a.N + tile - 1) / tile);
-    const int64_t unit = a.bf16 ? 64 : 32;
-    const int64_t steps = (a.K + unit - 1) / unit;
-    // two workgroups a CU, and at least eight steps each
-    int64_t splits = 512 / tiles;
-    if (splits > steps / 8) splits = steps / 8;
-    if (splits < 1) splits = 1;
+    const int64_t unit = a.bf16 ? 64 : 32, steps = (a.K + unit - 1) / unit;
+    auto tiles = [&](int m, int n) { return (a.M + m - 1) / m * ((a.N + n - 1) / n); };
+    const bool long_sum = steps >= (a.bf16 ? 64 : 128) && tiles(128, 128) >= 32;
+    a.tile_m = a.tile_n = 128;
+    if (tiles(128, 128) < (a.bf16 ? 512 : 192) && !long_sum) {
+        a.tile_n = 64;
+        if (tiles(128, 64) < 384)
+            a.tile_m = 64;
+    }
+    const int64_t count = tiles(a.tile_m, a.tile_n);
+    int64_t splits = 1;
+    if (count <= 128 && steps >= (a.bf16 ? 20 : 24)) {
+        splits = 512 / count;
+        if (splits > steps / (a.bf16 ? 4 : 6)) splits = steps / (a.bf16 ? 4 : 6);
+        if (splits > 16) splits = 16;
+    }
     const int64_t per = steps > 0 ? (steps + splits - 1) / splits : 1;
     a.split = per * unit;
     a.splits = steps > 0 ? (int32_t)((steps + per - 1) / per) : 1;
