@@ -255,7 +255,7 @@ def test_projection_nan_stays_in_its_row(dtype):
 LENGTHS = {"one": [1], "tile": [64], "tile + 1": [65], "mixed": [3, 0, 1, 64, 130], "equal": [70] * 3,
            "singles": [1] * 70, "late": [0, 0, 5], "long": [700, 300, 37], "even": [256] * 2}
 HEADS = [(1, 1, 1, 1), (2, 2, 16, 16), (3, 1, 64, 64), (4, 2, 48, 101), (2, 1, 128, 128),
-         (2, 2, 33, 64), (1, 1, 64, 128), (2, 1, 128, 17)]
+         (2, 2, 33, 64), (1, 1, 64, 128), (2, 1, 128, 17), (2, 1, 128, 64)]
 
 
 def packing(n):
@@ -419,12 +419,13 @@ def test_attention_decays_at_their_ends(dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("which", ["q", "k", "v", "dout"])
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])
-def test_a_token_does_not_reach_what_it_may_not(dtype, which, value):
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_a_token_does_not_reach_what_it_may_not(dtype, which, value, D):
     """A NaN or an infinity in one token: outputs before it, gradients of what it does not see, other
     heads and other sequences keep their bits or their values."""
     n, H, at = [100, 90], 2, 37
-    s, g = attention_inputs(n, H, 2, 32, 32, dtype, 6)
-    x = dict(s, dout=rand((190, H, 32), g, DTYPE[dtype]))
+    s, g = attention_inputs(n, H, 2, D, D, dtype, 6)
+    x = dict(s, dout=rand((190, H, D), g, DTYPE[dtype]))
     off = packing(n)
 
     def run(x):
