@@ -67,9 +67,6 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layer_norm_kernel(c
         col[j] = (j * LANES + lane) * 8;
         left[j] = a.D - col[j];
     }
-    float w[NV][8], b[NV][8];
-    load_vector<NV>(a.weight, col, left, 1.f, w);
-    load_vector<NV>(a.bias, col, left, 0.f, b);
     for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; row < a.T; row += stride) {
         float s[NV][8];
         load_sum<X, R, NV>(a, row, col, left, s);
@@ -82,6 +79,10 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layer_norm_kernel(c
                 sum[0] += s[j][i];
                 sum[1] += s[j][i] * s[j][i];
             }
+        // of each row's parameters a copy is in L1: kept in registers they would cost wavefronts
+        float w[NV][8], b[NV][8];
+        load_vector<NV>(a.weight, col, left, 1.f, w);
+        load_vector<NV>(a.bias, col, left, 0.f, b);
         row_sum<LANES>(sum, red, 1);
         const float rest = sum[0] * over_D;
         const float var = fmaxf(sum[1] * over_D - rest * rest, 0.f);
@@ -121,7 +122,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layer_norm_backward
     // beside a row, so each thread keeps its own in LDS
     constexpr bool KEEP = LANES * NV < 2048;
     __shared__ __align__(16) float kept[KEEP ? 1 : 2][KEEP ? 4 : NV * LANES * 8];
-    load_vector<NV>(a.weight, col, left, 1.f, w);
+    if constexpr (NV == 1)
+        load_vector<NV>(a.weight, col, left, 1.f, w);
     if constexpr (!KEEP)
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -139,6 +141,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layer_norm_backward
             load_some<8>(gp + col[j], left[j], g[j]);
             load_some<8>(dp ? dp + col[j] : dp, dp ? left[j] : 0, d[j]);
         }
+        if constexpr (NV > 1)  // two sums a feature beside it would leave room for fewer wavefronts
+            load_vector<NV>(a.weight, col, left, 1.f, w);
         centre<LANES, NV>(s, left, over_D, red);
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -228,18 +232,22 @@ template <typename X, typename R>
 hipError_t forward(const NormArgs &a, hipStream_t stream)
 {
     const Shape s = shape_of(a.D);
-    const dim3 grid((unsigned)block_count(a.T, s.rows, kBlocks)), block(s.lanes < 256 ? 256 : s.lanes);
+    const dim3 grid((unsigned)block_count(a.T, s.rows, kMostGroups)), block(s.lanes < 256 ? 256 : s.lanes);
     return by_shape(s, [&](auto lanes, auto nv) {
         layer_norm_kernel<X, R, decltype(lanes)::value, decltype(nv)::value>
             <<<grid, block, 0, stream>>>(a);
         return hipGetLastError();
     });
 }
+// Two sums a feature stay in registers, so rows above 4096 features get 1024 lanes.
+Shape backward_shape(int32_t D)
+{
+    return D > 4096 && D <= 8192 ? Shape{1024, 1, 1} : shape_of(D);
+}
 template <typename X, typename R> hipError_t backward(const NormArgs &a, hipStream_t stream)
 {
-    // two sums a feature stay in registers, so rows above 4096 features get 1024 lanes
-    const Shape s = a.D > 4096 && a.D <= 8192 ? Shape{1024, 1, 1} : shape_of(a.D);
-    const dim3 grid((unsigned)norm_partial_rows(a.T, a.D)), block(s.lanes < 256 ? 256 : s.lanes);
+    const Shape s = backward_shape(a.D);
+    const dim3 grid((unsigned)layer_norm_partial_rows(a.T, a.D)), block(s.lanes < 256 ? 256 : s.lanes);
     if (s.lanes == 1024 && s.nv == 1) {
         layer_norm_backward_kernel<X, R, 1024, 1><<<grid, block, 0, stream>>>(a);
         return hipGetLastError();
@@ -262,6 +270,14 @@ hipError_t launch_layer_norm(const NormArgs &a, bool bf16, bool residual_bf16, h
     return residual_bf16 ? forward<float, bf16_bits>(a, stream) : forward<float, float>(a, stream);
 }
 
+// As for the root-mean-square norm, with no more workgroups than the GPU holds at once.
+int64_t layer_norm_partial_rows(int64_t T, int32_t D)
+{
+    const Shape s = backward_shape(D);
+    const int64_t n = norm_partial_rows(T, D);
+    return s.nv > 1 && s.lanes < 1024 && n > 768 ? 768 : n;
+}
+
 hipError_t launch_layer_norm_backward(const NormArgs &a, float *dweight, float *dbias, bool bf16,
                                       bool residual_bf16, hipStream_t stream)
 {
@@ -276,7 +292,7 @@ hipError_t launch_layer_norm_backward(const NormArgs &a, float *dweight, float *
     }
     if (!dweight && !dbias)
         return hipSuccess;
-    return sum_rows(a.partial, a.T > 0 ? norm_partial_rows(a.T, a.D) : 0, 2 * (int64_t)a.D,
+    return sum_rows(a.partial, a.T > 0 ? layer_norm_partial_rows(a.T, a.D) : 0, 2 * (int64_t)a.D,
                     2 * (int64_t)a.D, ToWeightAndBias{dweight, dbias, a.D}, stream);
 }
 

@@ -208,7 +208,9 @@ lbi_status lbi_layer_norm(const void *x, int64_t ld_x, const void *residual, int
 
 size_t lbi_layer_norm_backward_workspace_bytes(int64_t T, int32_t D)
 {
-    return 2 * lbi_rms_norm_backward_workspace_bytes(T, D);
+    if (bad_norm_shape(T, D, 0.f) || T == 0)
+        return 0;
+    return (size_t)layer_norm_partial_rows(T, D) * 2 * D * sizeof(float);
 }
 
 lbi_status lbi_layer_norm_backward(const void *dout, int64_t ld_dout, const void *s, int64_t ld_s,

@@ -14,6 +14,7 @@ namespace lbi {
 // ---- layer norm (NormArgs)
 
 hipError_t launch_layer_norm(const NormArgs &a, bool bf16, bool residual_bf16, hipStream_t stream);
+int64_t layer_norm_partial_rows(int64_t T, int32_t D);  // of [2][D] partial sums
 hipError_t launch_layer_norm_backward(const NormArgs &a, float *dweight, float *dbias, bool bf16,
                                       bool residual_bf16, hipStream_t stream);
 

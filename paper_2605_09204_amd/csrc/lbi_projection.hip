@@ -197,8 +197,17 @@ template <int BM, int BN> __device__ __forceinline__ Place place(const ProductAr
     if (gridDim.x % 8 == 0)
         id = id % 8 * (gridDim.x / 8) + id / 8;
     Place x;
-    x.n0 = (int)(id % across) * BN;
-    const int64_t rest = first + id / across;
+    uint32_t column = id % across, row = id / across;
+    if (a.splits == 1) {
+        // eight rows of tiles at a time, so that what runs at once is a square of them
+        const uint32_t rows = gridDim.x / across, group = id / (8 * across);
+        const uint32_t high = rows - 8 * group < 8 ? rows - 8 * group : 8;
+        const uint32_t in_group = id - group * 8 * across;
+        row = 8 * group + in_group % high;
+        column = in_group / high;
+    }
+    x.n0 = (int)column * BN;
+    const int64_t rest = first + row;
     if (a.splits > 1) {  // few tiles: in 32 bits
         x.m0 = (int64_t)((uint32_t)rest / (uint32_t)a.splits) * BM;
         x.split = (int)((uint32_t)rest % (uint32_t)a.splits);
@@ -503,6 +512,17 @@ __global__ __launch_bounds__(256, 2) void product_dma_kernel(const ProductArgs a
                 for (int j = 0; j < NT; ++j)
                     mma(acc[i][j], fb[j], fa);
             }
+        }
+        if constexpr (sizeof(T) == 2) {
+            // the first half's operands, then the second half's among the first half's products
+            constexpr int READS = (A_COLS ? 2 : 1) * MT + (B_COLS ? 2 : 1) * NT, EACH = MT * NT / READS;
+            __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+#pragma unroll
+            for (int i = 0; i < READS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 2 * MT * NT - READS * EACH, 0);
         }
     }
     finish_rows<T, BM, BN, ACT>(a, acc, smem, at, wm, wn);
