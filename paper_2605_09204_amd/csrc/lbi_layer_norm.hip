@@ -67,6 +67,9 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layer_norm_kernel(c
         col[j] = (j * LANES + lane) * 8;
         left[j] = a.D - col[j];
     }
+    float w[NV][8], b[NV][8];
+    load_vector<NV>(a.weight, col, left, 1.f, w);
+    load_vector<NV>(a.bias, col, left, 0.f, b);
     for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; row < a.T; row += stride) {
         float s[NV][8];
         load_sum<X, R, NV>(a, row, col, left, s);
@@ -79,10 +82,6 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layer_norm_kernel(c
                 sum[0] += s[j][i];
                 sum[1] += s[j][i] * s[j][i];
             }
-        // of each row's parameters a copy is in L1: kept in registers they would cost wavefronts
-        float w[NV][8], b[NV][8];
-        load_vector<NV>(a.weight, col, left, 1.f, w);
-        load_vector<NV>(a.bias, col, left, 0.f, b);
         row_sum<LANES>(sum, red, 1);
         const float rest = sum[0] * over_D;
         const float var = fmaxf(sum[1] * over_D - rest * rest, 0.f);
@@ -232,7 +231,7 @@ template <typename X, typename R>
 hipError_t forward(const NormArgs &a, hipStream_t stream)
 {
     const Shape s = shape_of(a.D);
-    const dim3 grid((unsigned)block_count(a.T, s.rows, kMostGroups)), block(s.lanes < 256 ? 256 : s.lanes);
+    const dim3 grid((unsigned)block_count(a.T, s.rows, kBlocks)), block(s.lanes < 256 ? 256 : s.lanes);
     return by_shape(s, [&](auto lanes, auto nv) {
         layer_norm_kernel<X, R, decltype(lanes)::value, decltype(nv)::value>
             <<<grid, block, 0, stream>>>(a);

@@ -528,6 +528,87 @@ __global__ __launch_bounds__(256, 2) void product_dma_kernel(const ProductArgs a
     finish_rows<T, BM, BN, ACT>(a, acc, smem, at, wm, wn);
 }
 
+// ---- the product of few rows
+
+// 32 values k from k0 on of row `row`, straight from memory: bf16 8 g .., float32 4 g .. and 16 + 4 g ..
+template <typename T, bool PIECES> struct Direct {
+    Raw<T, 8> r;
+    __device__ __forceinline__ void load(const T *p, int64_t ld, int64_t row, int64_t rows, int k0,
+                                         int K)
+    {
+        const int g = threadIdx.x >> 4 & 3;
+        const T *at = p + (row < rows ? row : 0) * ld;
+        if constexpr (sizeof(T) == 2) {
+            const int k = k0 + 8 * g, left = row < rows ? K - k : 0;
+            r.load(at + k, PIECES ? (left > 0 ? 8 : 0) : left);
+        } else {
+            Raw<T, 4> x, y;
+            const int k = k0 + 4 * g, left = row < rows ? K - k : 0;
+            x.load(at + k, PIECES ? (left > 0 ? 4 : 0) : left);
+            y.load(at + k + 16, PIECES ? (left > 16 ? 4 : 0) : left - 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                r.v[i] = x.v[i];
+                r.v[4 + i] = y.v[i];
+            }
+        }
+    }
+    __device__ __forceinline__ void factor(Factor<T> &f) const
+    {
+        Frag<T> x;
+        if constexpr (sizeof(T) == 2) {
+            x.w = u4{r.w[0], r.w[1], r.w[2], r.w[3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                x.v[i] = r.v[i];
+        }
+        f.set(x);
+    }
+};
+
+// 16 rows by 16 columns to a workgroup, the sum dealt to eight wavefronts, operands from memory into
+// registers with everything of 2048 k in flight (float32: 1024), and one launch.  What a CU has in
+// flight from beyond L1 is what bounds it, so the work is spread over many.
+template <typename T, bool PIECES, int ACT>
+__global__ __launch_bounds__(512) void few_rows_kernel(const ProductArgs a)
+{
+    __shared__ f4 sums[8][64];
+    const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
+    const int across = (a.N + 15) / 16, n0 = blockIdx.x % across * 16, K = (int)a.K;
+    const int m0 = blockIdx.x / across * 16;
+    f4 acc = {0.f, 0.f, 0.f, 0.f};
+    // 64 values k to a wavefront at a time, in two steps
+    constexpr int DEEP = sizeof(T) == 4 ? 4 : 8, STEP = 8 * 64;
+    for (int k0 = wave * 64; k0 < K; k0 += STEP * DEEP / 2) {
+        Direct<T, PIECES> w[DEEP], x[DEEP];
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d) {
+            const int k = k0 + d / 2 * STEP + d % 2 * 32;
+            w[d].load((const T *)a.b, a.ld_b, n0 + c16, a.N, k, K);
+            x[d].load((const T *)a.a, a.ld_a, m0 + c16, a.M, k, K);
+        }
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d) {
+            Factor<T> fw, fx;
+            w[d].factor(fw);
+            x[d].factor(fx);
+            mma(acc, fw, fx);
+        }
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (wave > 0)
+        return;
+    f4 v = sums[0][lane];
+#pragma unroll
+    for (int k = 1; k < 8; ++k)
+        v += sums[k][lane];
+    const int m = m0 + c16, n = n0 + 4 * g;
+    if (m < a.M && n < a.N)
+        finish<T, ACT>(a, m, n, v);
+}
+
 // The sum of the splits' partial results, in order, through the epilogue.
 template <typename T, int ACT>
 __global__ __launch_bounds__(256) void join_kernel(const ProductArgs a)
@@ -627,9 +708,28 @@ hipError_t product(const ProductArgs &a, hipStream_t stream)
             product_kernel<T, A_COLS, B_COLS, BM, BN, ACT><<<grid, 256, 0, stream>>>(a, first);
     });
 }
+// Up to 64 rows, and no more workgroups than one or two a CU.  Onto 768 of 1536, bf16: 5.0 us at 64
+// rows (cut along the sum, in two launches: 7.8); onto 4096 of 4096: 10 at 16 rows, 31 at 64 (14).
+constexpr int kFewTiles = 384;
+bool few_rows(const ProductArgs &a)
+{
+    return !a.a_cols && !a.b_cols && a.M <= 64 && (a.M + 15) / 16 * ((a.N + 15) / 16) <= kFewTiles;
+}
+template <typename T, int ACT> hipError_t product_of_few(const ProductArgs &a, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((a.M + 15) / 16 * ((a.N + 15) / 16)));
+    if (in_pieces(a))
+        few_rows_kernel<T, true, ACT><<<grid, 512, 0, stream>>>(a);
+    else
+        few_rows_kernel<T, false, ACT><<<grid, 512, 0, stream>>>(a);
+    return hipGetLastError();
+}
 template <typename T, bool A_COLS, bool B_COLS, int ACT>
 hipError_t product_tiles(const ProductArgs &a, hipStream_t stream)
 {
+    if constexpr (!A_COLS && !B_COLS)
+        if (few_rows(a))
+            return product_of_few<T, ACT>(a, stream);
     if (a.tile_m == 64)
         return product<T, A_COLS, B_COLS, 64, 64, ACT>(a, stream);
     return a.tile_n == 64 ? product<T, A_COLS, B_COLS, 128, 64, ACT>(a, stream)
@@ -681,7 +781,7 @@ int64_t plan_product(ProductArgs &a)
     }
     const int64_t count = tiles(a.tile_m, a.tile_n);
     int64_t splits = 1;
-    if (count <= 128 && steps >= (a.bf16 ? 20 : 24)) {
+    if (!few_rows(a) && count <= 128 && steps >= (a.bf16 ? 20 : 24)) {
         splits = 512 / count;
         if (splits > steps / (a.bf16 ? 4 : 6)) splits = steps / (a.bf16 ? 4 : 6);
         if (splits > 16) splits = 16;

@@ -250,11 +250,14 @@ def _heads(name: str, t: torch.Tensor, lead, dtype, dev: int):
     if t.dtype is not dtype or t.get_device() != dev or shape[:k] != lead or len(shape) != k + 2:
         raise ValueError(f"{name} must be a {dtype} {(*lead, 'heads', 'values')} tensor on "
                          f"cuda:{dev}, got {t.dtype} {tuple(shape)} on {t.device}")
-    H, D = shape[k:]
-    if (D > 1 and stride[-1] != 1) or (H > 1 and stride[-2] != D):
+    H, D = shape[-2], shape[-1]
+    if (stride[-1] != 1 and D > 1) or (stride[-2] != D and H > 1):
         raise ValueError(f"{name}: a token's values must lie side by side")
-    return (_row_stride(name, (*lead, H * D), (*stride[:k], 1)), _int32(f"{name}'s heads", H),
-            _int32(f"{name}'s values", D))
+    if (H | D) >> 31:  # the library takes them in 32 bits
+        raise ValueError(f"{name}'s heads or values are out of range: {H}, {D}")
+    if k == 1:
+        return (stride[0] if lead[0] > 1 else H * D), H, D
+    return _row_stride(name, (*lead, H * D), (*stride[:k], 1)), H, D
 
 
 def _attention_inputs(q, k, v, log_decay, scale, offsets, sequences):

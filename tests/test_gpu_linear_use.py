@@ -326,7 +326,7 @@ def all_calls(seed=11, lengths=(700, 0, 3, 261)):
         return torch.randn(s, generator=g).to(dtype).to(DEV)
     f32, off = torch.float32, offsets_of(n)
     x, dy, w, b = r(T, D), r(T, D), r(D, dtype=f32), r(D, dtype=f32)
-    m, long, wide = r(D, D), r(40, 8000), r(96, 8000)
+    m, long, wide = r(D, D), r(100, 8000), r(96, 8000)
     pre, pre_out = r(T, D), torch.empty(T, D, dtype=torch.bfloat16, device=DEV)
     a = (r(T, H, DK), r(T, KH, DK), r(T, KH, DV), -torch.rand(H, generator=g).to(DEV))
     dout, st, dst = r(T, H, DV), r(S, H, DK, DV, dtype=f32), r(S, H, DK, DV, dtype=f32)
@@ -340,7 +340,7 @@ def all_calls(seed=11, lengths=(700, 0, 3, 261)):
         ("projection", lambda **k: (linear.lbi_projection(x, m, b, SILU, dy, pre=pre_out, **k),
                                     pre_out), linear.lbi_projection_workspace_bytes(T, D, D, bf)),
         ("projection in parts", lambda **k: (linear.lbi_projection(long, wide, **k),),
-         linear.lbi_projection_workspace_bytes(40, 8000, 96, bf)),
+         linear.lbi_projection_workspace_bytes(100, 8000, 96, bf)),
         ("projection backward", lambda **k: linear.lbi_projection_backward(x, m, dy, SILU, pre, **k),
          linear.lbi_projection_backward_workspace_bytes(T, D, D, SILU, bf, bf)),
         ("attention", lambda **k: (linear.lbi_linear_attention(*a, offsets=off, state_in=st,

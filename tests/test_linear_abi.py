@@ -97,13 +97,13 @@ def test_projection_refusals():
     assert projection(T=0, x=None, w=None, out=None) == 0
     # few rows and a long sum: cut into partial sums
     lib = linear.load()
-    need = lib.lbi_projection_workspace_bytes(64, 16384, 96, 1)
-    long = dict(T=64, K=16384, ldx=16384, ldw=16384)
-    if need:
-        assert projection(**long) == WORKSPACE
-        assert projection(ws=P[6], wsb=need - 1, **long) == WORKSPACE
-        assert projection(ws=P[6] + 8, wsb=need, **long) == ALIGN
-        assert projection(ws=P[4], wsb=need, **long) == ALIAS
+    need = lib.lbi_projection_workspace_bytes(100, 16384, 96, 1)
+    long = dict(T=100, K=16384, ldx=16384, ldw=16384)
+    assert need > 0
+    assert projection(**long) == WORKSPACE
+    assert projection(ws=P[6], wsb=need - 1, **long) == WORKSPACE
+    assert projection(ws=P[6] + 8, wsb=need, **long) == ALIGN
+    assert projection(ws=P[4], wsb=need, **long) == ALIAS
     assert lib.lbi_projection_workspace_bytes(0, 64, 64, 1) == 0
     assert lib.lbi_projection_workspace_bytes(64, 64, 64, 5) == 0
 
