@@ -708,12 +708,19 @@ hipError_t product(const ProductArgs &a, hipStream_t stream)
             product_kernel<T, A_COLS, B_COLS, BM, BN, ACT><<<grid, 256, 0, stream>>>(a, first);
     });
 }
-// Up to 64 rows, and no more workgroups than one or two a CU.  Onto 768 of 1536, bf16: 5.0 us at 64
-// rows (cut along the sum, in two launches: 7.8); onto 4096 of 4096: 10 at 16 rows, 31 at 64 (14).
+// Up to 64 rows, no more workgroups than one or two a CU, and a sum that one workgroup goes along
+// before two launches would be over: measured with 1 to 64 rows, 64 to 1536 columns and sums of
+// 1024 to 16384.  Onto 768 of 1536, bf16: 5.0 us at 64 rows (cut along the sum, in two launches:
+// 7.8); onto 64 of 16384 at 16 rows: 30 (14 in two launches); onto 1536 of 4096 at 64: 16 (13).
+// One row reads little beside the matrix, and float32's products take two to three times as long.
 constexpr int kFewTiles = 384;
 bool few_rows(const ProductArgs &a)
 {
-    return !a.a_cols && !a.b_cols && a.M <= 64 && (a.M + 15) / 16 * ((a.N + 15) / 16) <= kFewTiles;
+    if (a.a_cols || a.b_cols || a.M > 64)
+        return false;
+    const int64_t tiles = (a.M + 15) / 16 * ((a.N + 15) / 16);
+    return tiles <= kFewTiles &&
+           a.K * (tiles > 256 ? 2 : 1) * (a.M > 1 ? 3 : 2) <= (a.bf16 ? 16000 : 10500);
 }
 template <typename T, int ACT> hipError_t product_of_few(const ProductArgs &a, hipStream_t stream)
 {
