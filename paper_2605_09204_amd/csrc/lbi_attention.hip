@@ -28,6 +28,11 @@ template <typename T> constexpr int resident(int widths)
     return widths == 256 ? 1 : widths == 192 ? (sizeof(T) == 2 ? 2 : 1) : (sizeof(T) == 2 ? 3 : 2);
 }
 
+template <typename T> constexpr int resident_ends(int widths)
+{
+    return sizeof(T) == 2 || widths == 128 ? resident<T>(widths) : widths == 192 ? 3 : 2;
+}
+
 template <typename T, int DK, int DV, bool FULL>
 __global__ __launch_bounds__(256, resident<T>(DK + DV)) void attention_kernel(const AttentionArgs a, int64_t first)
 {
@@ -193,15 +198,21 @@ __global__ __launch_bounds__(256, resident<T>(DK + DV)) void attention_kernel(co
 // of the state of the sequence that passes its start.  With marks (the gradient's), also what the
 // range, or the sequence's first state, adds to the states before the second and further tiles of
 // each of its sequences.
+// both: every second workgroup goes backward, otherwise none does.
 template <typename T, int DK, int DV, bool FULL>
-__global__ __launch_bounds__(256, resident<T>(DK + DV)) void ends_kernel(const AttentionArgs a,
-                                                                        int64_t first, bool backward,
-                                                                        int tile_rows, int marks)
+__global__ __launch_bounds__(256, resident_ends<T>(DK + DV)) void ends_kernel(const AttentionArgs a,
+                                                                        int64_t first, bool both,
+                                                                        int mark_rows, int every)
 {
+    // Half a tile of float32 at 128 keys or values, of which the registers hold three workgroups a CU
+    // instead of one: 732 of them took 53 us, and 28 so.  (64 and 64: 59, and 64 so.)
+    constexpr int C = sizeof(T) == 4 && DK + DV >= 192 ? 32 : kAttentionTile;
     constexpr int QS = tile_stride<T>(DK), VS = tile_stride<T>(DV);
     __shared__ __align__(16) T tile_a[C * QS], tile_b[C * VS];
     const int h = blockIdx.x % a.in.H, kh = h / (a.in.H / a.in.KH);
-    const int64_t range = first + blockIdx.x / a.in.H;
+    const int64_t id = first + blockIdx.x / a.in.H, range = both ? id >> 1 : id;
+    const bool backward = both && (id & 1);
+    const int marks = backward ? 0 : every, tile_rows = marks > 0 ? mark_rows : C;
     const int dk = FULL ? DK : a.in.DK, dv = FULL ? DV : a.in.DV;
     const int64_t size = (int64_t)dk * dv, at = range * a.in.H + h;
     const float l2 = log2_decay(a.in.log_decay, h);
@@ -282,15 +293,18 @@ __global__ __launch_bounds__(256, resident<T>(DK + DV)) void ends_kernel(const A
 }
 
 // States along the ranges of a sequence (of all tokens, with offsets), or their gradients against
-// them: one thread for each value of each head.
+// them: one thread for V neighbouring values of a head, which lie at a multiple of V floats.
+template <int V>
 __global__ __launch_bounds__(256) void carry_kernel(const AttentionArgs a, int64_t first,
-                                                    int blocks, bool backward)
+                                                    int blocks, bool both)
 {
+    typedef float fv __attribute__((ext_vector_type(V)));
     const int64_t size = (int64_t)a.in.DK * a.in.DV;
     const uint32_t id = blockIdx.x;
-    const int64_t e = (int64_t)(id % blocks) * 256 + threadIdx.x;
+    const int64_t e = ((int64_t)(id % blocks) * 256 + threadIdx.x) * V;
     const int h = id / blocks % a.in.H;
-    const int64_t chain = first + id / blocks / a.in.H;
+    const int64_t which = first + id / blocks / a.in.H, chain = both ? which >> 1 : which;
+    const bool backward = both && (which & 1);
     if (e >= size)
         return;
     const int64_t count = a.cut.per_sequence > 0 ? a.cut.per_sequence : a.cut.ranges;
@@ -301,27 +315,35 @@ __global__ __launch_bounds__(256) void carry_kernel(const AttentionArgs a, int64
     const int64_t last = backward ? 0 : count - 1, way = backward ? -1 : 1;
     float *at = p + (chain * count + (count - 1 - last)) * step;
     flags += chain * count + (count - 1 - last);
-    float v = 0.f;
-    // sixteen ranges are loaded at once, whether something passes them or not
-    constexpr int AHEAD = 16;
-    for (int64_t left = count; left > 0; left -= AHEAD) {
-        float x[AHEAD];
+    // the next ranges are on their way before this step's stores, whether something passes them or not
+    constexpr int AHEAD = V == 4 ? 4 : 8;
+    fv v = 0.f, next[AHEAD];
+    int32_t next_flag[AHEAD];
+    auto load = [&](int64_t done) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int64_t to = (done + k < count ? done + k : count - 1) * way;
+            next_flag[k] = flags[to];
+            next[k] = *(const fv *)(at + to * step);
+        }
+    };
+    load(0);
+    for (int64_t done = 0; done < count; done += AHEAD) {
+        fv x[AHEAD];
         int32_t f[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-            if (k < left) {
-                f[k] = flags[k * way];
-                x[k] = at[k * way * step];
-            }
+        for (int k = 0; k < AHEAD; ++k) {
+            x[k] = next[k];
+            f[k] = next_flag[k];
+        }
+        if (done + AHEAD < count)
+            load(done + AHEAD);
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-            if (k < left) {
-                v = f[k] == kWhole ? x[k] + fade * v : x[k];
-                if (f[k] == kWhole)
-                    at[k * way * step] = v;
-            }
-        at += AHEAD * way * step;
-        flags += AHEAD * way;
+        for (int k = 0; k < AHEAD; ++k) {
+            v = f[k] == kWhole ? x[k] + fade * v : x[k];
+            if (f[k] == kWhole && done + k < count)
+                *(fv *)(at + (done + k) * way * step) = v;
+        }
     }
 }
 
@@ -421,9 +443,9 @@ __global__ __launch_bounds__(256) void step_kernel(const AttentionArgs a, int64_
 // for the forward pass, where a round is what the GPU holds at once, a workgroup costs two tiles
 // besides its own, forming the states that ranges add takes half of a walk with outputs, and
 // carrying them three tile times and more for each 32 ranges; the gradient's walk counts twice, and
-// so does what comes before it.  Measured against ranges of 64 to 2048 tokens, 14 calls of 1500
-// to 33000 tokens, the forward pass in bf16 and float32 and the gradient: within 6 per cent of the
-// best of them, except for long float32 calls (8) and 30 short sequences' gradients (9).
+// the states before it are formed for both sides at once.  Measured against ranges of 64 to 1024
+// tokens, 12 gradients of 2271 to 31948 tokens: within 7 per cent of the best of them, one (36 heads
+// of 16, three sequences) 12.  Forward, bf16 and float32: within 8.
 AttentionCut attention_cut(const lbi_attention_inputs &in, bool ragged, bool backward)
 {
     AttentionCut best = {};
@@ -431,8 +453,9 @@ AttentionCut attention_cut(const lbi_attention_inputs &in, bool ragged, bool bac
         return best;
     const int widths = (in.DK <= 64 ? 64 : 128) + (in.DV <= 64 ? 64 : 128);
     const bool bf16 = in.dt == LBI_BF16;
-    const int64_t ends_slots = 256 * (bf16 ? resident<bf16_bits>(widths) : resident<float>(widths));
-    const int64_t slots = !backward ? ends_slots : bf16 && widths == 128 ? 512 : 256;
+    const int64_t ends_slots = 256 * (bf16 ? resident_ends<bf16_bits>(widths) : resident_ends<float>(widths));
+    const int64_t slots = backward ? (widths <= (bf16 ? 128 : 192) ? 512 : 256)
+                                   : 256 * (bf16 ? resident<bf16_bits>(widths) : resident<float>(widths));
     const int64_t len = ragged ? in.T : in.T / in.sequences;
     const int64_t most = (len + kAttentionTile - 1) / kAttentionTile;
     double least = 0;
@@ -446,10 +469,14 @@ AttentionCut attention_cut(const lbi_attention_inputs &in, bool ragged, bool bac
         c.per_sequence = ragged ? 0 : (int32_t)per;
         c.joined = per > 1;
         const double groups = (double)c.ranges * in.H;
-        auto rounds = [&](int64_t n) { return (double)((int64_t)((groups + n - 1) / n)); };
-        const double walk = rounds(slots) * (tiles + 2), ends = 0.5 * rounds(ends_slots) * (tiles + 2);
-        const double cost = (backward ? 2 * walk + ends : walk) +
-                            (c.joined ? ends + 3 + (double)per / 32 : 0);
+        auto rounds = [&](double groups, int64_t n) {
+            return (double)((int64_t)((groups + n - 1) / n)) * (double)(tiles + 2);
+        };
+        const double walk = rounds(groups, slots), ends = rounds(groups, ends_slots) / 2;
+        const double join = 3 + (double)per / 32;
+        const double cost = !backward    ? walk + (c.joined ? ends + join : 0)
+                            : !c.joined ? 2 * walk + ends
+                                        : 2 * walk + rounds(2 * groups, ends_slots) / 2 + join;
         if (tiles == 1 || cost < least) {
             least = cost;
             best = c;
@@ -459,23 +486,30 @@ AttentionCut attention_cut(const lbi_attention_inputs &in, bool ragged, bool bac
     }
 }
 
-hipError_t launch_attention_ends(const AttentionArgs &a, bool backward, int tile_rows, int marks,
+// Both sides of the gradient go in one launch, which fills the GPU better than one after the other:
+// 46 us instead of 52 (8 sequences of 2048 tokens, 12 heads of 64, bf16).
+hipError_t launch_attention_ends(const AttentionArgs &a, bool both, int mark_rows, int marks,
                                  hipStream_t stream)
 {
+    const int64_t sides = both ? 2 : 1;
     hipError_t e = by_head(a.in, [&](auto type, auto dk, auto dv, auto full) {
-        return in_launches(a.cut.ranges, a.in.H, [&](int64_t first, dim3 grid) {
+        return in_launches(a.cut.ranges * sides, a.in.H, [&](int64_t first, dim3 grid) {
             ends_kernel<decltype(type), decltype(dk)::value, decltype(dv)::value,
                         decltype(full)::value>
-                <<<grid, 256, 0, stream>>>(a, first, backward, tile_rows, marks);
+                <<<grid, 256, 0, stream>>>(a, first, both, mark_rows, marks);
         });
     });
     if (e != hipSuccess || !a.cut.joined)
         return e;
     const int64_t size = (int64_t)a.in.DK * a.in.DV;
-    const int blocks = (int)((size + 255) / 256);
-    const int64_t chains = a.cut.per_sequence > 0 ? a.in.sequences : 1;
+    const int64_t chains = (a.cut.per_sequence > 0 ? a.in.sequences : 1) * sides;
+    // four values to a thread where that leaves each CU its 256: 96 chains of 4 or 5 states of 4096
+    // values take 6 us so, 10 one by one; 12 chains of about 200 took 16, one by one 9
+    const bool wide = size % 4 == 0 && chains * a.in.H * (size / 4) >= 256 * 256;
+    const int blocks = (int)((size / (wide ? 4 : 1) + 255) / 256);
     return in_launches(chains, (int64_t)blocks * a.in.H, [&](int64_t first, dim3 grid) {
-        carry_kernel<<<grid, 256, 0, stream>>>(a, first, blocks, backward);
+        if (wide) carry_kernel<4><<<grid, 256, 0, stream>>>(a, first, blocks, both);
+        else carry_kernel<1><<<grid, 256, 0, stream>>>(a, first, blocks, both);
     });
 }
 
@@ -491,7 +525,7 @@ hipError_t launch_linear_attention(const AttentionArgs &a, hipStream_t stream)
     hipError_t e = hipSuccess;
     if (a.in.T > 0) {
         if (a.cut.joined)
-            e = launch_attention_ends(a, false, C, 0, stream);
+            e = launch_attention_ends(a, false, 0, 0, stream);
         if (e == hipSuccess)
             e = by_head(a.in, [&](auto type, auto dk, auto dv, auto full) {
                 return in_launches(a.cut.ranges, a.in.H, [&](int64_t first, dim3 grid) {

@@ -22,12 +22,13 @@
 namespace lbi {
 namespace {
 
-// Tokens of a tile: 64, or 32 where four float32 tiles of 128 values would not fit in LDS.
+// Tokens of a tile: 64, or 32 of float32, of which LDS and the registers hold two workgroups a CU
+// (heads of 256 values together: one), not one.  3885 tokens, 6 heads of 48 and 101: 131 us -> 88.
 template <typename T, int DK, int DV>
-constexpr int tile_tokens() { return sizeof(T) == 4 && DK + DV == 256 ? 32 : 64; }
+constexpr int tile_tokens() { return sizeof(T) == 4 ? 32 : 64; }
 
 template <typename T, int DK, int DV, bool FULL>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && DK + DV == 128 ? 2 : 1) void
+__global__ __launch_bounds__(256, DK + DV <= (sizeof(T) == 2 ? 128 : 192) ? 2 : 1) void
 attention_backward_kernel(const AttentionArgs a, int64_t first, int marks)
 {
     constexpr int C = tile_tokens<T, DK, DV>();
@@ -384,16 +385,20 @@ attention_backward_kernel(const AttentionArgs a, int64_t first, int marks)
         a.part_decay[range * a.in.H + h] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
-// The gradients of shared keys and values: the sums over the heads that share them.
+// The gradients of shared keys and values: the sums over the heads that share them.  The first half of
+// the workgroups has the keys', the second the values'.
 template <typename T>
-__global__ __launch_bounds__(256) void shared_heads_kernel(const float *part, T *out, int64_t ld,
-                                                           int64_t T0, int64_t count, int KH,
-                                                           int share, int width)
+__global__ __launch_bounds__(256) void shared_heads_kernel(const AttentionArgs a)
 {
-    const int64_t per = (int64_t)KH * width;
-    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < count * per;
-         id += (int64_t)gridDim.x * 256) {
-        const int64_t t = T0 + id / per;
+    const bool values = blockIdx.x >= gridDim.x / 2;
+    const int width = values ? a.in.DV : a.in.DK, KH = a.in.KH, share = a.in.H / KH;
+    const float *part = values ? a.part_v : a.part_k;
+    T *out = (T *)(values ? a.out.dv : a.out.dk);
+    const int64_t ld = values ? a.out.ld_dv : a.out.ld_dk;
+    const int64_t per = (int64_t)KH * width, blocks = gridDim.x / 2;
+    for (int64_t id = (values ? blockIdx.x - blocks : blockIdx.x) * 256 + threadIdx.x;
+         id < a.in.T * per; id += blocks * 256) {
+        const int64_t t = id / per;
         const int at = (int)(id % per), kh = at / width, d = at % width;
         const float *p = part + (t * KH + kh) * share * width + d;
         float v = p[0];
@@ -426,10 +431,9 @@ hipError_t launch_linear_attention_backward(const AttentionArgs &a, hipStream_t 
     hipError_t e = hipSuccess;
     if (a.in.T > 0) {
         const int marks = (int)attention_marks(a.in, a.cut);
-        const int tile_rows = (int)(a.cut.tokens / marks);
-        e = launch_attention_ends(a, false, tile_rows, marks, stream);
-        if (e == hipSuccess && a.cut.joined)
-            e = launch_attention_ends(a, true, kAttentionTile, 0, stream);
+        if (a.cut.joined || marks > 1)  // the first tile has none
+            e = launch_attention_ends(a, a.cut.joined, (int)(a.cut.tokens / marks), marks,
+                                      stream);
         if (e == hipSuccess)
             e = by_head(a.in, [&](auto type, auto dk, auto dv, auto full) {
                 using T = decltype(type);
@@ -441,20 +445,13 @@ hipError_t launch_linear_attention_backward(const AttentionArgs &a, hipStream_t 
         if (e != hipSuccess)
             return e;
         if (a.part_k) {
-            const int share = a.in.H / a.in.KH;
-            auto sum = [&](auto type, const float *part, void *out, int64_t ld, int width) {
-                using T = decltype(type);
-                const int64_t n = (a.in.T * a.in.KH * width + 255) / 256;
-                shared_heads_kernel<T><<<dim3((unsigned)(n < 8192 ? n : 8192)), 256, 0, stream>>>(
-                    part, (T *)out, ld, 0, a.in.T, a.in.KH, share, width);
-            };
-            if (a.in.dt == LBI_BF16) {
-                sum(bf16_bits{}, a.part_k, a.out.dk, a.out.ld_dk, a.in.DK);
-                sum(bf16_bits{}, a.part_v, a.out.dv, a.out.ld_dv, a.in.DV);
-            } else {
-                sum(float{}, a.part_k, a.out.dk, a.out.ld_dk, a.in.DK);
-                sum(float{}, a.part_v, a.out.dv, a.out.ld_dv, a.in.DV);
-            }
+            const int width = a.in.DK > a.in.DV ? a.in.DK : a.in.DV;
+            const int64_t n = (a.in.T * a.in.KH * width + 255) / 256;
+            const dim3 grid(2 * (unsigned)(n < 4096 ? n : 4096));
+            if (a.in.dt == LBI_BF16)
+                shared_heads_kernel<bf16_bits><<<grid, 256, 0, stream>>>(a);
+            else
+                shared_heads_kernel<float><<<grid, 256, 0, stream>>>(a);
             e = hipGetLastError();
         }
     }

@@ -105,9 +105,9 @@ enum : int32_t { kPart = 1, kWhole = 2 };
 hipError_t launch_linear_attention(const AttentionArgs &a, hipStream_t stream);
 hipError_t launch_linear_attention_step(const AttentionArgs &a, hipStream_t stream);
 hipError_t launch_linear_attention_backward(const AttentionArgs &a, hipStream_t stream);
-// The states at the ranges' ends, or (backward) their gradients at the ranges' starts; with marks, the
-// states before tiles of tile_rows tokens, as far as the range they are in adds to them.
-hipError_t launch_attention_ends(const AttentionArgs &a, bool backward, int tile_rows, int marks,
+// The states at the ranges' ends and, for both, their gradients at the ranges' starts; with marks,
+// also the states before tiles of mark_rows tokens, as far as the range they are in adds to them.
+hipError_t launch_attention_ends(const AttentionArgs &a, bool both, int mark_rows, int marks,
                                  hipStream_t stream);
 // States (or their gradients) of sequences without tokens.
 hipError_t launch_attention_empty(const AttentionArgs &a, bool backward, hipStream_t stream);
