@@ -91,7 +91,10 @@ typedef enum {
  *             same pointer as residual (with the same stride).
  *   pre       OUTPUT [T][N] dt: z, for the gradient; or NULL (not written).
  *   T >= 0, 1 <= K, N <= LBI_PROJECTION_MAX (else LBI_ERR_SHAPE).
- * dt float32: every product in float32, on the fp32 matrix cores.
+ * dt float32: a value goes into the products as the sum of three bf16 values,
+ * of whose nine products six are added in float32: at most 2^-22 of a product is
+ * left out.  Below 2^-110 the smaller parts begin to vanish; a value of 3.395e38
+ * and more, or an infinity, gives NaN where it is a factor.
  * A NaN or an infinity stays within its row of x, or its row of the weight.
  *   workspace  lbi_projection_workspace_bytes(T, K, N, dt) bytes, 256-byte
  *              aligned (NULL where that is 0): partial sums of calls whose
@@ -113,7 +116,7 @@ lbi_status lbi_projection(const void *x, int64_t ld_x, const void *weight, int64
  *   dweight    OUTPUT [N][K] dt, at row stride ld_dweight: dz^T x; or NULL.
  *   dbias      OUTPUT [N] float32: the sum over rows of dz; or NULL.
  * dz is formed in float32; as an operand of the two products it is rounded to
- * dt.  All sums are float32.
+ * dt, and float32 products are as above.  All sums are float32.
  *   workspace  lbi_projection_backward_workspace_bytes(...) bytes, 256-byte
  *              aligned (NULL where that is 0).
  */
@@ -164,7 +167,9 @@ typedef struct {
  * Tokens are taken in chunks: within one by the products of queries and keys,
  * across them by the state, which is float32.  With bf16 tokens the products of
  * queries and keys are rounded to bf16 before they meet the values; a state
- * meets the queries as the sum of two bf16 values (at most 2^-16 away).
+ * meets the queries as the sum of two bf16 values (at most 2^-16 away).  A NaN
+ * or an infinity in a token reaches no earlier token; one in a state gives a NaN
+ * or an infinity in its column, from there on.
  */
 size_t lbi_linear_attention_workspace_bytes(int64_t T, int64_t sequences, int32_t H, int32_t KH,
                                             int32_t DK, int32_t DV, int32_t ragged, lbi_dtype dt);

@@ -2,7 +2,7 @@
 
 Usage: ``python -m paper_2605_09204_amd.build`` (or ``build_library()``).
 Cross-compiles without a GPU.  Each translation unit under ``csrc/`` (one per
-arithmetic mode of the chain kernel, the carry/apply kernels, the region block's
+arithmetic mode of the chain kernel, the carry/apply kernels, the region blocks'
 operators, the host API) is
 compiled in parallel, then linked.  Packed fp32 instructions are disabled for
 all device code.

@@ -126,7 +126,7 @@ __device__ __forceinline__ void mma(f4 &acc, const Frag<float> &a, const Frag<fl
 // A float32 operand.  For the bf16 matrix cores it is a sum of bf16 values, for one product each:
 // three are the value itself (what two round to nearest leave has at most 8 significant bits) and
 // go into states, which are results in float32; two leave at most 2^-16 of it, a random rounding,
-// and take a state into products with tokens.
+// and take a state into the outputs' and the values' gradients' products with tokens.
 template <typename T, int PARTS> struct Wide;
 template <int PARTS> struct Wide<bf16_bits, PARTS> {
     Frag<bf16_bits> part[PARTS];

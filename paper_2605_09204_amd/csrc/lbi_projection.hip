@@ -7,6 +7,11 @@
 // (forward), of one (dx) or of none (dW).  A workgroup takes a BM x BN tile of the result, the
 // operands pass through LDS as they lie, and the matrix instructions' operands are read from there
 // straight or through the transposing read.
+//
+// bf16, 16384 x 768 onto 1536 takes 49 us (790 TFLOP/s), 58 with SiLU and z written; 4096^3 124 us
+// (1110).  Between the barriers of two stages the matrix cores wait for LDS; a tile of 128 x 128 is
+// what two workgroups a CU, which fill those waits, leave registers for.  float32 4096^3: 730 us (188),
+// bound by the vector ALUs that split the operands beside the matrix cores.
 #include "lbi_attention.hpp"
 #include "lbi_dma.hpp"
 
@@ -388,8 +393,6 @@ __device__ __forceinline__ void stage_operand(Frag<T> &f, uint32_t stage, int ti
     }
 }
 
-// Two stages: one on its way while the other is worked on.  (Five of half their depth were slower by a
-// fifth: what a step costs besides its loads outweighs their latency.)
 // Eight sums of a row of the result, n .. n + 7, through the epilogue.
 template <typename T, typename O, int ACT>
 __device__ __forceinline__ void finish_eight(const ProductArgs &a, int64_t m, int n, float (&v)[8])
@@ -416,8 +419,9 @@ __device__ __forceinline__ void finish_eight(const ProductArgs &a, int64_t m, in
             v[i] += r[i];
     store_some<8>((O *)a.out + m * a.ld_out + n, left, v);
 }
-// The workgroup's tile through LDS, where the wavefronts' results become whole rows, and out: stores
-// of 8 bytes from where the results are took twice as long.  A row's 16-byte pieces are exchanged by
+// The workgroup's tile through LDS, where the wavefronts' results become whole rows, and out: with
+// stores of 8 bytes from where the results are, 16384 x 1536 bf16 results and their z took 34 us
+// behind a sum of 64, and 25 so.  A row's 16-byte pieces are exchanged by
 // its number, so that 16 rows' pieces of one column lie in different banks.
 template <typename T, int BM, int BN, int ACT, int MT, int NT>
 __device__ __forceinline__ void finish_rows(const ProductArgs &a, const f4 (&acc)[MT][NT], char *smem,
@@ -456,6 +460,8 @@ __device__ __forceinline__ void finish_rows(const ProductArgs &a, const f4 (&acc
     }
 }
 
+// Two stages: one on its way while the other is worked on.  (Five of half their depth were slower by a
+// fifth: what a step costs besides its loads outweighs their latency.)
 template <typename T, bool A_COLS, bool B_COLS, int BM, int BN, int ACT>
 __global__ __launch_bounds__(256, 2) void product_dma_kernel(const ProductArgs a, int64_t first)
 {

@@ -22,6 +22,7 @@ LBI_ACT_GELU = 2
 LBI_PROJECTION_MAX = 65536
 LBI_ATTENTION_MAX_DIM = 128
 LBI_ATTENTION_MAX_H = 1024
+LBI_ATTENTION_MAX_LD = 1 << 23
 
 
 class AttentionInputs(ctypes.Structure):
@@ -277,7 +278,7 @@ def _attention_inputs(q, k, v, log_decay, scale, offsets, sequences):
     return AttentionInputs(
         q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v,
         _vector("log_decay", log_decay, (H,), dev), None, _ptr(offsets), T, n, H, KH, DK, DV,
-        DK ** -0.5 if scale is None else float(scale), _DTYPES[dtype]), lead, dtype, dev
+        max(DK, 1) ** -0.5 if scale is None else float(scale), _DTYPES[dtype]), lead, dtype, dev
 
 
 def _output(name, out, like, shape, dtype, dev: int):

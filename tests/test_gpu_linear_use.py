@@ -522,3 +522,13 @@ def test_example():
     diff = attention_block.serve()
     say(f"[example] serving: {diff:.2g}")
     assert diff <= 2e-2
+
+
+@gpu
+def test_heads_without_values_are_refused():
+    q = torch.zeros(5, 1, 0, dtype=torch.bfloat16, device=DEV)
+    v, decay = torch.zeros(5, 1, 4, dtype=torch.bfloat16, device=DEV), torch.zeros(1, device=DEV)
+    with pytest.raises(binding.LbiError):
+        linear.lbi_linear_attention(q, q, v, decay)
+    with pytest.raises(binding.LbiError):
+        linear.lbi_linear_attention_backward(q, q, v, decay, v)

@@ -41,6 +41,8 @@ def test_limits_match_the_header():
     text = open(HEADER).read()
     for name in ("LBI_PROJECTION_MAX", "LBI_ATTENTION_MAX_DIM", "LBI_ATTENTION_MAX_H"):
         assert int(re.search(rf"#define {name} (\d+)", text).group(1)) == getattr(linear, name)
+    shift = re.search(r"#define LBI_ATTENTION_MAX_LD \(1 << (\d+)\)", text).group(1)
+    assert 1 << int(shift) == linear.LBI_ATTENTION_MAX_LD
     for name in ("LBI_ACT_NONE", "LBI_ACT_SILU", "LBI_ACT_GELU"):
         assert int(re.search(rf"{name} = (\d+)", text).group(1)) == getattr(linear, name)
 
