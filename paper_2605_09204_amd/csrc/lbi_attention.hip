@@ -384,7 +384,8 @@ __global__ __launch_bounds__(256) void empty_kernel(const AttentionArgs a, int64
 }
 
 // One token: a workgroup takes a head of a sequence, COLS lanes of 4 columns side by side, the
-// other lanes further rows.  Bound by the state, which is read and written once.
+// other lanes further rows.  Bound by the state, which is read and written once: 64 sequences, 12 heads
+// of 64 and 128, 50 MB, take 11 us (a copy of that total 7.5).
 template <typename T, int COLS>
 __global__ __launch_bounds__(256) void step_kernel(const AttentionArgs a, int64_t first)
 {

@@ -18,10 +18,10 @@
 // held in both layouts, as the operand of G v and of G^T k.  The states that enter the ranges and
 // the gradients that leave them are carried as in the forward pass.
 //
-// 8 sequences of 2048 tokens, 12 heads of 64, bf16: 88 to 98 us for the walk (226 MB with the kept
-// states), 37 for both sides of the ranges, 6 for the carry.  The walk waits half of its cycles, on
-// LDS (a sixth of it bank conflicts) and on products in a chain, at the two workgroups a CU that its
-// registers leave.
+// 8 sequences of 2048 tokens, 12 heads of 64, bf16: 96 to 99 us for the walk (226 MB with the kept
+// states), 37 for both sides of the ranges, 6 for the carry.  The walk's wavefronts wait half of
+// their cycles, on LDS (39 per cent of its cycles are bank conflicts) and on products in a chain, at
+// the two workgroups a CU that the registers leave.
 #include "lbi_attention.hpp"
 
 namespace lbi {
