@@ -45,8 +45,9 @@ extern "C" {
  *                 var(s) = mean((s - mean(s))^2) and s in float32 (not yet rounded).
  *   T >= 0, 1 <= D <= LBI_NORM_MAX_D, eps >= 0 (else LBI_ERR_SHAPE).
  * A row of equal values gives bias (eps > 0); a NaN or an infinity gives NaN in
- * its row.  The sum of the squares is float32: where it passes that range
- * (differences of 10^19 / sqrt(D) and more) finite values give bias.
+ * its row, as does a difference from the mean that float32 does not hold.  The
+ * sum of the squares is float32: where it passes that range (differences of
+ * 10^19 / sqrt(D) and more) finite values give bias, and a gradient of dresidual.
  */
 lbi_status lbi_layer_norm(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual,
                           const float *weight, const float *bias, void *out, int64_t ld_out,

@@ -9,6 +9,10 @@
 // formed over its lanes, and HBM is the bound.  The mean comes first, then the squares of the
 // differences from it, so nothing cancels where the mean is far from zero; the differences'
 // own mean, what the first one's rounding left, is taken off in the same sums.
+// The mean is the row's first value and the mean of the distances from it: equal values, whose
+// variance would otherwise be what roundings leave, have differences of exactly zero.  Terms are
+// divided by D before they are added, so no sum but that of the squares leaves float32's range;
+// where that one does, 1 / sqrt is 0 and the row gives its bias.
 // Everything is float32 until the one rounding to the output's type.
 //
 // 16384 x 768 bf16 with a residual: 18.5 us (101 MB, 5.4 TB/s: a copy's rate).  The gradient at
@@ -20,24 +24,49 @@
 namespace lbi {
 namespace {
 
-// s -> s - mean for the row's features, 0 behind them.
+// The value of the row's first lane.  slot: LDS that the row's sums do not use.
+template <int LANES> __device__ __forceinline__ float of_first_lane(float x, float *slot)
+{
+    if constexpr (LANES == 64) {
+        return bitsf(__builtin_amdgcn_readfirstlane(fbits(x)));
+    } else if constexpr (LANES < 64) {
+        return __shfl(x, 0, LANES);
+    } else {
+        if (threadIdx.x == 0)
+            *slot = x;
+        __syncthreads();  // two more until the next row writes it
+        return bitsf(__builtin_amdgcn_readfirstlane(fbits(*slot)));
+    }
+}
+
+// s -> s - mean for the row's features, 0 behind them.  Halves keep the distances in range.
 template <int LANES, int NV>
 __device__ __forceinline__ void centre(float (&s)[NV][8], const int (&left)[NV], float over_D,
                                        float *red)
 {
+    const float first = of_first_lane<LANES>(s[0][0], red + (LANES > 64 ? LANES / 64 : 0));
+    const float half = 0.5f * first;
     float sum[1] = {0.f};
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            sum[0] += s[j][i];
+            sum[0] = fmaf(i < left[j] ? fmaf(0.5f, s[j][i], -half) : 0.f, over_D, sum[0]);
     row_sum<LANES>(sum, red, 0);
-    const float mean = sum[0] * over_D;
+    const float mean = fmaf(2.f, sum[0], first);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             s[j][i] = i < left[j] ? s[j][i] - mean : 0.f;
+}
+
+// 1 / sqrt(var + eps) from the squares' sum and the differences' mean: 0 for an infinite sum (the
+// square of the rest alone might be infinite too), NaN for a NaN and an infinite difference.
+__device__ __forceinline__ float reciprocal_root(float squares, float over_D, float rest, float eps)
+{
+    const float var = fmaf(-rest, rest, squares * over_D);
+    return rsqrtf((var < 0.f ? 0.f : var) + eps);
 }
 
 template <int NV>
@@ -83,14 +112,11 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layer_norm_kernel(c
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                sum[0] += s[j][i];
+                sum[0] = fmaf(s[j][i], over_D, sum[0]);
                 sum[1] += s[j][i] * s[j][i];
             }
         row_sum<LANES>(sum, red, 1);
-        const float rest = sum[0] * over_D;
-        const float var = fmaxf(sum[1] * over_D - rest * rest, 0.f);
-        // fmaxf drops a NaN
-        const float r = rsqrtf((sum[1] == sum[1] ? var : sum[1]) + a.eps);
+        const float rest = sum[0], r = reciprocal_root(sum[1], over_D, rest, a.eps);
         X *o = (X *)a.out + row * a.ld_out;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -107,7 +133,13 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layer_norm_backward
     const NormArgs a)
 {
     constexpr int ROWS = LANES < 256 ? 256 / LANES : 1, W = LANES > 64 ? LANES / 64 : 1;
-    __shared__ float red[8 * W];
+    // rows above 8192 features: the registers do not hold the sums of the parameters' gradients
+    // beside a row, so each thread keeps its own in LDS (behind the row's sums: addresses past 64 KB
+    // would take a register each)
+    constexpr bool KEEP = LANES * NV < 2048;
+    constexpr int SUMS = KEEP ? 0 : NV * LANES * 8;
+    __shared__ __align__(16) float red[8 * W + 2 * SUMS];
+    float *const kept[2] = {red + 8 * W, red + 8 * W + SUMS};
     const int lane = threadIdx.x % LANES;
     const int64_t stride = (int64_t)gridDim.x * ROWS;
     const float over_D = 1.f / (float)a.D;
@@ -121,10 +153,6 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layer_norm_backward
         for (int i = 0; i < 8; ++i)
             dw[j][i] = db[j][i] = 0.f;
     }
-    // rows above 8192 features: the registers do not hold the sums of the parameters' gradients
-    // beside a row, so each thread keeps its own in LDS
-    constexpr bool KEEP = LANES * NV < 2048;
-    __shared__ __align__(16) float kept[KEEP ? 1 : 2][KEEP ? 4 : NV * LANES * 8];
     if constexpr (NV == 1)
         load_vector<NV>(a.weight, col, left, 1.f, w);
     if constexpr (!KEEP)
@@ -153,17 +181,16 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layer_norm_backward
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float gw = g[j][i] * w[j][i];
-                sum[0] += s[j][i];
+                sum[0] = fmaf(s[j][i], over_D, sum[0]);
                 sum[1] += s[j][i] * s[j][i];
                 sum[2] += gw;
                 sum[3] += gw * s[j][i];
             }
         row_sum<LANES>(sum, red, 1);
-        const float rest = sum[0] * over_D;
-        const float var = fmaxf(sum[1] * over_D - rest * rest, 0.f);
-        const float r = rsqrtf((sum[1] == sum[1] ? var : sum[1]) + a.eps);
+        const float rest = sum[0], r = reciprocal_root(sum[1], over_D, rest, a.eps);
         const float mean_g = sum[2] * over_D;
-        const float mean_gn = (sum[3] - rest * sum[2]) * r * over_D;
+        // 0 with an r of 0, where the last sum may have left the range
+        const float mean_gn = r > 0.f ? (sum[3] - rest * sum[2]) * r * over_D : 0.f;
         R *o = (R *)a.out + row * a.ld_out;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -273,7 +300,8 @@ hipError_t launch_layer_norm(const NormArgs &a, bool bf16, bool residual_bf16, h
     return residual_bf16 ? forward<float, bf16_bits>(a, stream) : forward<float, float>(a, stream);
 }
 
-// As for the root-mean-square norm, with no more workgroups than the GPU holds at once.
+// As for the root-mean-square norm, but three workgroups a CU for rows of 513 to 4096 features: what
+// the GPU holds at once above 1024 (registers); up to there it would hold four.
 int64_t layer_norm_partial_rows(int64_t T, int32_t D)
 {
     const Shape s = backward_shape(D);
