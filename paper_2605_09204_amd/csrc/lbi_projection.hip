@@ -745,8 +745,10 @@ hipError_t product_tiles(const ProductArgs &a, hipStream_t stream)
             return product_of_few<T, ACT>(a, stream);
     if (a.tile_m == 64)
         return product<T, A_COLS, B_COLS, 64, 64, ACT>(a, stream);
-    return a.tile_n == 64 ? product<T, A_COLS, B_COLS, 128, 64, ACT>(a, stream)
-                          : product<T, A_COLS, B_COLS, 128, 128, ACT>(a, stream);
+    if constexpr (sizeof(T) == 2)
+        if (a.tile_n == 64)
+            return product<T, A_COLS, B_COLS, 128, 64, ACT>(a, stream);
+    return product<T, A_COLS, B_COLS, 128, 128, ACT>(a, stream);
 }
 template <typename T> hipError_t product_by(const ProductArgs &a, hipStream_t stream)
 {
@@ -776,8 +778,9 @@ template <typename T> hipError_t product_by(const ProductArgs &a, hipStream_t st
 //
 // The larger a tile, the fewer bytes and (float32) splits a product takes, but two workgroups a CU
 // are needed to keep it busy: 128 x 128 from 512 tiles on (float32: 192, its steps being three times
-// as long), 128 x 64 from 384.  bf16, 2048 x 2048 x 2048: 31 us with 256 tiles, 27 with 512, 28 with
-// 1024; 16384 x 1536 x 768: 55, 57, 66; float32, 4099 x 768 x 1536: 86, 93, 107.
+// as long), 128 x 64 from 384 (bf16 alone: fewer than 192 of 128 x 128 never make as many).  bf16,
+// 2048 x 2048 x 2048: 31 us with 256 tiles, 27 with 512, 28 with 1024; 16384 x 1536 x 768: 55, 57,
+// 66; float32, 4099 x 768 x 1536: 86, 93, 107.
 // Fewer tiles than 128 are cut along the sum to about two workgroups a CU, where each keeps at least
 // 4 steps (float32: 6) of 20 (24): the second launch costs 3 us and the partial sums' traffic.
 // bf16, 512 x 512 x 4096: 34 us whole, 14 in eight; 6707 x 64 x 1104: 10 whole, 11 in two.
@@ -789,7 +792,7 @@ int64_t plan_product(ProductArgs &a)
     a.tile_m = a.tile_n = 128;
     if (tiles(128, 128) < (a.bf16 ? 512 : 192) && !long_sum) {
         a.tile_n = 64;
-        if (tiles(128, 64) < 384)
+        if (!a.bf16 || tiles(128, 64) < 384)
             a.tile_m = 64;
     }
     const int64_t count = tiles(a.tile_m, a.tile_n);

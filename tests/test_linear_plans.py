@@ -74,3 +74,11 @@ DWEIGHT = [((200, 4104, 2056), WHOLE, WHOLE), ((203, 4101, 2055), WHOLE, WHOLE),
 def test_products_take_their_tiles(plan, cases):
     for sizes, bf16, f32 in cases:
         assert plan(*sizes, BF16) == bf16 and plan(*sizes, F32) == f32, sizes
+
+
+def test_float32_products_have_no_tiles_of_128_by_64():
+    """Fewer than 192 tiles of 128 x 128 are fewer than 384 of 128 x 64."""
+    for M in range(1, 6000, 61):
+        for N in range(1, 6000, 57):
+            for K in (100, 5000):
+                assert product_plan(M, K, N, F32)[:2] in ((128, 128), (64, 64))
