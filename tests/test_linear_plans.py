@@ -82,3 +82,25 @@ def test_float32_products_have_no_tiles_of_128_by_64():
         for N in range(1, 6000, 57):
             for K in (100, 5000):
                 assert product_plan(M, K, N, F32)[:2] in ((128, 128), (64, 64))
+
+
+class AttentionCut(ctypes.Structure):
+    """AttentionCut of csrc/lbi_linear_internal.h."""
+
+    _fields_ = [("ranges", ctypes.c_int64), ("tokens", ctypes.c_int64),
+                ("per_sequence", ctypes.c_int32), ("joined", ctypes.c_bool)]
+
+
+def attention_plan(lengths, H, KH, DK, DV, dt, backward):
+    """(tiles of 64 tokens a range, ranges, whether states pass between ranges, values a thread of the
+    carry)."""
+    cut = getattr(linear.load(), "_ZN3lbi13attention_cutERK20lbi_attention_inputsbb")
+    cut.argtypes = [ctypes.POINTER(linear.AttentionInputs), ctypes.c_bool, ctypes.c_bool]
+    cut.restype = AttentionCut
+    ragged = len(set(lengths)) > 1
+    a = linear.AttentionInputs(T=sum(lengths), sequences=len(lengths), H=H, KH=KH, DK=DK, DV=DV,
+                               dt=dt)
+    c = cut(ctypes.byref(a), ragged, backward)
+    chains = (1 if ragged else len(lengths)) * (2 if backward else 1)
+    wide = DK * DV % 4 == 0 and chains * H * DK * DV // 4 >= 256 * 256
+    return c.tokens // 64, c.ranges, c.joined, (4 if wide else 1) if c.joined else 0
