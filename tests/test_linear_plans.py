@@ -104,3 +104,28 @@ def attention_plan(lengths, H, KH, DK, DV, dt, backward):
     chains = (1 if ragged else len(lengths)) * (2 if backward else 1)
     wide = DK * DV % 4 == 0 and chains * H * DK * DV // 4 >= 256 * 256
     return c.tokens // 64, c.ranges, c.joined, (4 if wide else 1) if c.joined else 0
+
+
+# Lengths, H, KH, DK, DV, whose ranges of several tiles pass states on, forward and in the gradient, in
+# both types: heads that fill the tiles' widths and heads that do not, equal sequences, one, and packed
+# ones that begin in the middle of a range or last over several; both forms of the carry.
+PACKED = [300, 1, 0, 1203, 64]
+RANGES = [([520] * 3, 54, 18, 64, 64), (PACKED, 66, 22, 64, 64), ([1500], 72, 72, 64, 64),
+          (PACKED, 48, 48, 48, 101), ([900] * 2, 36, 12, 48, 101), ([1500], 48, 48, 48, 101),
+          (PACKED, 66, 22, 40, 56), (PACKED, 24, 8, 128, 128), ([700] * 2, 24, 24, 128, 128),
+          (PACKED, 48, 48, 64, 128), (PACKED, 48, 48, 128, 64)]
+
+
+def test_attention_is_cut_into_ranges_of_several_tiles():
+    carries = {False: set(), True: set()}
+    for lengths, H, KH, DK, DV in RANGES:
+        for dt in (F32, BF16):
+            for backward in (False, True):
+                tiles, ranges, joined, carry = attention_plan(lengths, H, KH, DK, DV, dt, backward)
+                assert joined and tiles >= 3 and ranges >= 4, (lengths, H, DK, DV, dt, backward)
+                carries[backward].add((carry, len(set(lengths)) > 1))
+    # the gradient's carry of single values is that of few heads (test_gpu_linear_use.py)
+    assert carries[False] >= {(1, True), (4, True), (4, False), (1, False)}
+    assert carries[True] >= {(4, True), (4, False)}
+    for lengths in ([5001], [4100, 31, 1500, 0, 900]):
+        assert attention_plan(lengths, 1, 1, 12, 20, BF16, True)[2:] == (True, 1)
