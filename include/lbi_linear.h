@@ -168,9 +168,10 @@ typedef struct {
  * Tokens are taken in chunks: within one by the products of queries and keys,
  * across them by the state, which is float32.  With bf16 tokens the products of
  * queries and keys are rounded to bf16 before they meet the values; a state
- * meets the queries as the sum of two bf16 values (at most 2^-16 away).  A NaN
- * or an infinity in a token reaches no earlier token; one in a state gives a NaN
- * or an infinity in its column, from there on.
+ * meets the queries as the sum of two bf16 values (at most 2^-16 away; NaN for a
+ * value of 3.395e38 and more, which bf16 does not hold).  A NaN or an infinity in
+ * a token reaches no earlier token; one in a state gives a NaN or an infinity in
+ * its column, from there on.
  */
 size_t lbi_linear_attention_workspace_bytes(int64_t T, int64_t sequences, int32_t H, int32_t KH,
                                             int32_t DK, int32_t DV, int32_t ragged, lbi_dtype dt);
@@ -196,6 +197,9 @@ typedef struct {
  *
  *   dout        [T][H][DV] dt.
  *   dstate_out  [sequences][H][DK][DV] float32: gradient of state_out, or NULL.
+ * With bf16 tokens the products over pairs of tokens are rounded to bf16 as
+ * operands for dq, dk and dv; states and their gradients enter dq and dk as three
+ * bf16 values and dv as two.  dlog_decay is formed from what is not yet rounded.
  */
 size_t lbi_linear_attention_backward_workspace_bytes(int64_t T, int64_t sequences, int32_t H,
                                                      int32_t KH, int32_t DK, int32_t DV,

@@ -20,8 +20,10 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 // ---- matrix operands
 
 // Tiles of bf16 in LDS have the two halves of every 16 values exchanged in rows 8 .. 15 of 16, at
-// a stride of 32 bytes more than their values: the 32 lanes that LDS serves together then touch
-// all its banks once, reading rows and reading columns.  Float32 tiles lie as they are.
+// a stride of 32 bytes more than their values: 32 lanes that read 8 bytes each, of rows or of columns,
+// then name all 64 banks once.  Stores of rows and reads of columns have no conflicts (ends_kernel has
+// nothing else, and the counter is 0 there); the walks, which also read rows and store p and e, have
+// them in 40 per cent of their LDS cycles (64 and 64).  Float32 tiles lie as they are.
 template <typename T> __device__ __forceinline__ int swapped(int row)
 {
     return sizeof(T) == 2 ? row & 8 : 0;

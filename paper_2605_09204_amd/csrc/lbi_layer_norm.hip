@@ -17,7 +17,7 @@
 //
 // 16384 x 768 bf16 with a residual: 18.5 us (101 MB, 5.4 TB/s: a copy's rate).  The gradient at
 // 12289 x 768 bf16 on a float32 stream (132 MB): 26 us and 4 for the parameters' sums, one row after
-// the other at few wavefronts a SIMD.
+// the other at three wavefronts a SIMD.
 #include "lbi_linear_internal.h"
 #include "lbi_norm_rows.hpp"
 
